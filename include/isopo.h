@@ -501,6 +501,22 @@ typedef struct {
 size_t isopo_linear_workspace(int64_t n_tokens, int32_t d_in, int32_t d_out, isopo_dtype dtype);
 size_t isopo_linear_backward_workspace(int64_t n_tokens, int32_t d_in, int32_t d_out, isopo_dtype dtype);
 
+/* How such a layer's product (backward non-zero: dX of isopo_linear_backward) is launched.  Host arithmetic only.  A product of more tiles
+ * than a launch holds is cut into launches of whole tokens, one behind the other; `first_token` names the launch that is asked
+ * for: 0, or the token at which the one before ends.
+ *   tokens         of this launch
+ *   tile           tokens and outputs of a workgroup's tile
+ *   sum_waves      waves that form a tile's sum in as many parts, joined in the workgroup; 1: all waves share its blocks
+ *   parts          into which workgroups split the sum, through the workspace; 1 where the product is cut
+ *   workspace_end  bytes from the call's workspace on that this launch's parts reach to; 0: it has none */
+typedef struct {
+  int64_t tokens;
+  int32_t tile, sum_waves, parts;
+  size_t workspace_end;
+} isopo_linear_plan_info;
+isopo_status isopo_linear_plan(int64_t n_tokens, int32_t d_in, int32_t d_out, isopo_dtype dtype, int32_t backward, int64_t first_token,
+                               isopo_linear_plan_info* plan);
+
 /* Y [n_tokens, d_out], rows ldy apart.  Z: dense [n_tokens, d_out] for the backward pass, or NULL.  Y and Z may not overlap X, W, each
  * other or (but for Y = residual) the residual.  Bit-identical from run to run. */
 isopo_status isopo_linear(const isopo_linear_layer* layer, void* Y, void* Z, void* workspace, size_t ws_bytes, void* stream);

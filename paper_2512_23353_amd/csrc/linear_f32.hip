@@ -543,27 +543,24 @@ __global__ __launch_bounds__(256) void linear_f32_parts_kernel(LinearArgs a, con
 }
 
 enum class Tile { k128, k64, k64By4, k64By8 };      // By: by waves that split the sum
-struct SplitPlan {
-  Tile tile;
-  int parts, blocks_per_part;
-};
 constexpr int side_of(Tile t) { return t == Tile::k128 ? 128 : 64; }
+constexpr int sum_waves_of(Tile t) { return t == Tile::k64By4 ? 4 : t == Tile::k64By8 ? 8 : 1; }
 
 // Tiles and parts of a product: the smallest modelled time, in microseconds.  A workgroup costs a start and, per block or block of each wave, what
 // it takes of its compute unit: 128 x 128 tiles, three to a unit, 2 and 0.64 (alone 0.75); 64 x 64, 1 and 0.23 (alone 0.3); by four waves that split
 // the sum 2.5 (alone 1.5) and 0.79; by eight, where none waits for a unit, 1.5 and 1.45.  Parts cost a second launch, 0.12 each and the workspace's
 // traffic at 8 bytes per output and part (a little much beside the kernels' time, as the second launch costs the host more).  With 4 us for the
 // launch it is 14 % below to 28 % above what was measured on 40 products of 1 .. 40000 tokens.
-SplitPlan plan(long long rows, int k, int n_out) {
+LinearPlan plan(long long rows, int k, int n_out, bool may_split) {
   const int blocks = (k + kTerms - 1) / kTerms;
   const double outputs = (double)rows * n_out;
-  SplitPlan best = {Tile::k128, 1, blocks};
+  LinearPlan best = {rows, 128, 1, 1, blocks};
   double least = 1e300;
   for (const Tile tile : {Tile::k128, Tile::k64, Tile::k64By4, Tile::k64By8}) {
     const int side = side_of(tile);
     const double tiles = (double)((rows + side - 1) / side) * ((n_out + side - 1) / side);
     for (const int want : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64}) {
-      if (want > 1 && (want > blocks / 4 || tiles * want > 2048.0)) break;
+      if (want > 1 && (!may_split || want > blocks / 4 || tiles * want > 2048.0)) break;
       const int per = (blocks + want - 1) / want, parts = (blocks + per - 1) / per;
       const double wgs = tiles * parts, rounds = wgs <= 768.0 ? std::ceil(wgs / 256.0) : wgs / 256.0;
       const bool alone = wgs <= 256.0;
@@ -575,7 +572,7 @@ SplitPlan plan(long long rows, int k, int n_out) {
       const double time = one * rounds + (parts > 1 ? 3.0 + parts * (0.12 + outputs * 1e-6) : 0.0);
       if (time < least) {
         least = time;
-        best = {tile, parts, per};
+        best = {rows, side, sum_waves_of(tile), parts, per};
       }
     }
   }
@@ -606,25 +603,20 @@ hipError_t launch_wave(const SplitParams& p, unsigned blocks, hipStream_t s) {
 }
 
 template <bool TERM_ROWS>
-hipError_t launch_plan(const SplitParams& p, Tile tile, unsigned blocks, hipStream_t s) {
-  if (tile == Tile::k128) return launch_split<2, 1, TERM_ROWS>(p, blocks, s);
-  if (tile == Tile::k64) return launch_split<1, 2, TERM_ROWS>(p, blocks, s);
-  return tile == Tile::k64By4 ? launch_wave<4, TERM_ROWS>(p, blocks, s) : launch_wave<8, TERM_ROWS>(p, blocks, s);
+hipError_t launch_plan(const SplitParams& p, const LinearPlan& pl, unsigned blocks, hipStream_t s) {
+  if (pl.side == 128) return launch_split<2, 1, TERM_ROWS>(p, blocks, s);
+  if (pl.sum_waves == 1) return launch_split<1, 2, TERM_ROWS>(p, blocks, s);
+  return pl.sum_waves == 4 ? launch_wave<4, TERM_ROWS>(p, blocks, s) : launch_wave<8, TERM_ROWS>(p, blocks, s);
 }
 
 }  // namespace
 
-size_t linear_split_workspace(long long rows, int k, int n_out) {
-  const SplitPlan pl = plan(rows, k, n_out);
-  return pl.parts > 1 ? (size_t)pl.parts * rows * n_out * sizeof(float) : 0;
-}
+LinearPlan linear_split_plan(long long rows, int k, int n_out, bool may_split) { return plan(rows, k, n_out, may_split); }
 
-hipError_t launch_linear_split(const LinearArgs& a, hipStream_t s) {
-  const SplitPlan pl = plan(a.rows, a.k, a.n_out);
+hipError_t launch_linear_split(const LinearArgs& a, const LinearPlan& pl, hipStream_t s) {
   SplitParams p;
   p.a = a;
-  const int side = side_of(pl.tile);
-  const long long mt = (a.rows + side - 1) / side, nt = (a.n_out + side - 1) / side;
+  const long long mt = (a.rows + pl.side - 1) / pl.side, nt = (a.n_out + pl.side - 1) / pl.side;
   if (mt * nt * pl.parts > 0x7fffffffLL) return hipErrorInvalidValue;
   p.grid = tile_grid((int)mt, (int)nt);
   p.tiles = (int)(mt * nt);
@@ -632,7 +624,7 @@ hipError_t launch_linear_split(const LinearArgs& a, hipStream_t s) {
   p.parts = pl.parts > 1 ? a.workspace : nullptr;
   p.workgroups = (unsigned)(p.tiles * pl.parts);
   const unsigned blocks = p.workgroups + row_sum_blocks(a.then);
-  const hipError_t e = a.b_rows_are_k ? launch_plan<true>(p, pl.tile, blocks, s) : launch_plan<false>(p, pl.tile, blocks, s);
+  const hipError_t e = a.b_rows_are_k ? launch_plan<true>(p, pl, blocks, s) : launch_plan<false>(p, pl, blocks, s);
   if (e != hipSuccess || pl.parts == 1) return e;
   const long long threads = a.rows * a.n_out / 4;
   with_act(a.act, [&](auto act) {

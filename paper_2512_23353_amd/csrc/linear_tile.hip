@@ -347,28 +347,24 @@ __global__ __launch_bounds__(256) void linear_parts_kernel(LinearArgs a, const f
   *reinterpret_cast<u32x4*>(static_cast<u16*>(a.C) + row * a.ldc + col) = pack8(z);
 }
 
-struct TilePlan {
-  int side, parts, blocks_per_part;
-};
-
 // Tiles and parts of a product: the smallest modelled time, in microseconds.  A workgroup costs a start and, per block, what it takes of its compute
 // unit: 256 x 256 tiles, one to a unit, 5 and 1.2; 128 x 128, two to a unit, 2 and 0.5 (two together 1.7 times one).  Parts cost a second
 // launch, 0.12 each and the workspace's traffic at 8 bytes per output and part.  Within 10 % of what was measured on 16 products of 1 .. 14119 tokens, 2 to
 // 12 points each; what the model takes is at most 8 % from the best of them.
-TilePlan plan(long long rows, int k, int n_out) {
+LinearPlan plan(long long rows, int k, int n_out, bool may_split) {
   const auto tiles = [&](int b) { return (double)((rows + b - 1) / b) * ((n_out + b - 1) / b); };
   const int blocks = (k + kTerms - 1) / kTerms;
   const double big = (5.0 + 1.2 * blocks) * std::ceil(tiles(256) / 256.0), small = tiles(128), outputs = (double)rows * n_out;
-  TilePlan best = {256, 1, blocks};
+  LinearPlan best = {rows, 256, 1, 1, blocks};
   double least = big;
   for (const int want : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64}) {
-    if (want > 1 && (want > blocks / 2 || small * want > 2048.0)) break;
+    if (want > 1 && (!may_split || want > blocks / 2 || small * want > 2048.0)) break;
     const int per = (blocks + want - 1) / want, parts = (blocks + per - 1) / per;
     const double wgs = small * parts, rounds = wgs <= 256.0 ? 1.0 : wgs <= 512.0 ? 1.7 : wgs / 256.0;
     const double time = (2.0 + 0.5 * per) * rounds + (parts > 1 ? 3.0 + parts * (0.12 + outputs * 1e-6) : 0.0);
     if (time < least) {
       least = time;
-      best = {128, parts, per};
+      best = {rows, 128, 1, parts, per};
     }
   }
   return best;
@@ -386,19 +382,15 @@ hipError_t launch(const TileParams& p, unsigned blocks, hipStream_t s) {
 }
 
 template <bool TERM_ROWS>
-hipError_t launch_plan(const TileParams& p, const TilePlan& pl, unsigned blocks, hipStream_t s) {
+hipError_t launch_plan(const TileParams& p, const LinearPlan& pl, unsigned blocks, hipStream_t s) {
   return pl.side == 256 ? launch<256, 256, 2, 4, 2, TERM_ROWS>(p, blocks, s) : launch<128, 128, 2, 2, 2, TERM_ROWS>(p, blocks, s);
 }
 
 }  // namespace
 
-size_t linear_tile_workspace(long long rows, int k, int n_out) {
-  const TilePlan pl = plan(rows, k, n_out);
-  return pl.parts > 1 ? (size_t)pl.parts * rows * n_out * sizeof(float) : 0;
-}
+LinearPlan linear_tile_plan(long long rows, int k, int n_out, bool may_split) { return plan(rows, k, n_out, may_split); }
 
-hipError_t launch_linear_tile(const LinearArgs& a, hipStream_t s) {
-  const TilePlan pl = plan(a.rows, a.k, a.n_out);
+hipError_t launch_linear_tile(const LinearArgs& a, const LinearPlan& pl, hipStream_t s) {
   TileParams p;
   p.a = a;
   const long long mt = (a.rows + pl.side - 1) / pl.side, nt = (a.n_out + pl.side - 1) / pl.side;

@@ -36,14 +36,23 @@ struct LinearArgs {
   float* workspace;
   RowSum then;                 // formed by workgroups of the same launch behind the product's
 };
-size_t linear_workspace(long long rows, int k, int n_out, bool bf16, bool b_rows_are_k);
+// One launch of a product.
+struct LinearPlan {
+  long long rows;              // its rows
+  int side;                    // outputs and tokens of a tile
+  int sum_waves;               // waves that split a tile's sum (1: they share its blocks)
+  int parts, blocks_per_part;  // of the sum, by different workgroups; parts 1: it is whole
+};
+// The launch that starts at row `first` (0, or where the launch before ends).
+LinearPlan linear_plan(long long rows, int k, int n_out, bool bf16, long long first);
+size_t linear_workspace(const LinearPlan& p, int n_out);
 hipError_t launch_linear(const LinearArgs& a, hipStream_t s);
-// bf16, tiles of 128 or 256 outputs and tokens (launch_linear routes to it)
-size_t linear_tile_workspace(long long rows, int k, int n_out);
-hipError_t launch_linear_tile(const LinearArgs& a, hipStream_t s);
+// bf16, tiles of 128 or 256 outputs and tokens (launch_linear routes to it).  may_split false: there is no workspace for parts.
+LinearPlan linear_tile_plan(long long rows, int k, int n_out, bool may_split);
+hipError_t launch_linear_tile(const LinearArgs& a, const LinearPlan& pl, hipStream_t s);
 // fp32, tiles of 64 or 128
-size_t linear_split_workspace(long long rows, int k, int n_out);
-hipError_t launch_linear_split(const LinearArgs& a, hipStream_t s);
+LinearPlan linear_split_plan(long long rows, int k, int n_out, bool may_split);
+hipError_t launch_linear_split(const LinearArgs& a, const LinearPlan& pl, hipStream_t s);
 
 // Delta = dY act'(Z) (NULL: not written) and its column sums (db NULL: none).  *rest: NULL, or set to what is left to sum for db.
 struct ActBackwardArgs {

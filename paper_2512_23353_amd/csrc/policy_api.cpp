@@ -59,12 +59,30 @@ extern "C" {
 
 size_t isopo_linear_workspace(int64_t n_tokens, int32_t d_in, int32_t d_out, isopo_dtype dtype) {
   if (check_shape(n_tokens, d_in, d_out, dtype) != ISOPO_OK || n_tokens == 0) return 0;
-  return linear_workspace(n_tokens, d_in, d_out, dtype == ISOPO_BF16, false);
+  return linear_workspace(linear_plan(n_tokens, d_in, d_out, dtype == ISOPO_BF16, 0), d_out);
 }
 
 size_t isopo_linear_backward_workspace(int64_t n_tokens, int32_t d_in, int32_t d_out, isopo_dtype dtype) {
   if (check_shape(n_tokens, d_in, d_out, dtype) != ISOPO_OK || n_tokens == 0) return 0;
-  return align_up(act_backward_workspace(n_tokens, d_out)) + linear_workspace(n_tokens, d_out, d_in, dtype == ISOPO_BF16, true);
+  return align_up(act_backward_workspace(n_tokens, d_out)) + linear_workspace(linear_plan(n_tokens, d_out, d_in, dtype == ISOPO_BF16, 0), d_in);
+}
+
+isopo_status isopo_linear_plan(int64_t n_tokens, int32_t d_in, int32_t d_out, isopo_dtype dtype, int32_t backward, int64_t first_token,
+                               isopo_linear_plan_info* plan) {
+  const isopo_status st = check_shape(n_tokens, d_in, d_out, dtype);
+  if (st != ISOPO_OK) return st;
+  if (!plan || first_token < 0 || first_token >= n_tokens) return ISOPO_ERR_INVALID_ARG;
+  const int k = backward ? d_out : d_in, n_out = backward ? d_in : d_out;
+  const LinearPlan head = linear_plan(n_tokens, k, n_out, dtype == ISOPO_BF16, 0);
+  if (first_token % head.rows) return ISOPO_ERR_INVALID_ARG;
+  const LinearPlan p = linear_plan(n_tokens, k, n_out, dtype == ISOPO_BF16, first_token);
+  plan->tokens = p.rows;
+  plan->tile = p.side;
+  plan->sum_waves = p.sum_waves;
+  plan->parts = p.parts;
+  plan->workspace_end = linear_workspace(p, n_out);
+  if (backward && p.parts > 1) plan->workspace_end += align_up(act_backward_workspace(n_tokens, d_out));
+  return ISOPO_OK;
 }
 
 isopo_status isopo_linear(const isopo_linear_layer* l, void* Y, void* Z, void* workspace, size_t ws_bytes, void* stream) {

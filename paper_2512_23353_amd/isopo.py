@@ -43,7 +43,7 @@ EXPORTS = ("isopo_layer_step", "isopo_layer_gram_plan", "isopo_gram_cost_model",
            "isopo_fisher_samples_block_workspace", "isopo_fisher_samples_block",
            "isopo_weighted_grad_scratch", "isopo_weighted_grad_prescaled",
            "isopo_gram_norms", "isopo_rescale", "isopo_ntk_eigh_workspace", "isopo_ntk_eigh",
-           "isopo_linear_workspace", "isopo_linear_backward_workspace", "isopo_linear", "isopo_linear_backward",
+           "isopo_linear_workspace", "isopo_linear_backward_workspace", "isopo_linear_plan", "isopo_linear", "isopo_linear_backward",
            "isopo_token_logprob", "isopo_token_logprob_backward",
            "isopo_grad_norm_workspace", "isopo_grad_norm", "isopo_adamw", "isopo_adamw_clipped", "isopo_adamw_state",
            "isopo_transform_eigh", "isopo_probe_mfma_loop", "isopo_probe_lds_dma", "isopo_probe_contraction_waves", "isopo_status_string", "isopo_version")
@@ -184,6 +184,8 @@ def load() -> ctypes.CDLL:
     lib.isopo_linear_workspace.restype = sz
     lib.isopo_linear_backward_workspace.argtypes = [i64, i32, i32, ctypes.c_int]
     lib.isopo_linear_backward_workspace.restype = sz
+    lib.isopo_linear_plan.argtypes = [i64, i32, i32, ctypes.c_int, i32, i64, vp]
+    lib.isopo_linear_plan.restype = ctypes.c_int
     lib.isopo_linear.argtypes = [ctypes.POINTER(_LinearLayer), vp, vp, vp, sz, vp]
     lib.isopo_linear.restype = ctypes.c_int
     lib.isopo_linear_backward.argtypes = [vp, i64, vp, vp, ctypes.c_int, ctypes.c_int, i64, i32, i32, vp, vp, vp, vp, sz, vp]
@@ -695,6 +697,22 @@ def _linear_workspace(n: int, d_in: int, d_out: int, dtype: int) -> int:
 @functools.lru_cache(maxsize=4096)
 def _linear_backward_workspace(n: int, d_in: int, d_out: int, dtype: int) -> int:
     return int(load().isopo_linear_backward_workspace(n, d_in, d_out, dtype))
+
+
+class LinearPlanInfo(ctypes.Structure):
+    _fields_ = [("tokens", ctypes.c_int64), ("tile", ctypes.c_int32), ("sum_waves", ctypes.c_int32), ("parts", ctypes.c_int32),
+                ("workspace_end", ctypes.c_size_t)]
+
+
+def linear_plan(n: int, d_in: int, d_out: int, dtype: int, backward: bool = False) -> list:
+    """The launches of a linear layer's product, or of its backward pass's dX, first to last (host arithmetic only)."""
+    out, first = [], 0
+    while first < n:
+        info = LinearPlanInfo()
+        _check(load().isopo_linear_plan(n, d_in, d_out, dtype, int(bool(backward)), first, ctypes.byref(info)), "isopo_linear_plan")
+        out.append({name: getattr(info, name) for name, _ in LinearPlanInfo._fields_})
+        first += info.tokens
+    return out
 
 
 def _act(act: str) -> int:
