@@ -14,12 +14,12 @@ namespace {
 constexpr int kVecs = 32, kRows = 8;
 constexpr int kOneChunk = 128;           // up to so many rows one workgroup's sums are db's: no second launch
 // rows of a chunk: enough chunks to fill the chip, not so many that their sums weigh
-int chunk_rows(long long rows, int cols) {
+long long chunk_rows(long long rows, int cols) {
   if (rows <= kOneChunk) return kOneChunk;
   const long long wide = (cols + 255) / 256;
   long long c = (rows * wide + 1023) / 1024;
   c = (c + kRows - 1) / kRows * kRows;
-  return (int)(c < 64 ? 64 : c);
+  return c < 64 ? 64 : c;
 }
 long long chunks_of(long long rows, int cols) { return (rows + chunk_rows(rows, cols) - 1) / chunk_rows(rows, cols); }
 
@@ -32,7 +32,7 @@ __device__ __forceinline__ V load(const void* at) {
 
 struct Params {
   ActBackwardArgs a;
-  int chunk;
+  long long chunk;
 };
 
 // ONCE: dY and Z are read for the last time and need not be kept in the caches.
@@ -43,7 +43,7 @@ __global__ __launch_bounds__(256) void act_backward_kernel(Params p) {
   const ActBackwardArgs& a = p.a;
   const int vec = threadIdx.x % kVecs, row = threadIdx.x / kVecs;
   const int col = (blockIdx.x * kVecs + vec) * V;
-  const long long r0 = (long long)blockIdx.y * p.chunk, r1 = r0 + p.chunk < a.rows ? r0 + p.chunk : a.rows;
+  const long long r0 = blockIdx.y * p.chunk, r1 = r0 + p.chunk < a.rows ? r0 + p.chunk : a.rows;
   float sum[V] = {};
   if (col < a.cols) {
     for (long long r = r0 + row; r < r1; r += kRows) {

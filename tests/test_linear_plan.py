@@ -65,3 +65,13 @@ def test_plan_refuses():
     for i, bad, status in ((0, -1, 1), (0, 0, 1), (0, 1 << 31, 3), (1, 12, 3), (1, 0, 1), (2, 4, 3), (3, 5, 3), (5, -1, 1), (5, 256, 1), (5, 1 << 22, 1), (6, None, 1)):
         assert lib.isopo_linear_plan(*ok[:i], bad, *ok[i + 1:]) == status, (i, bad)
     assert isopo.linear_plan(0, 64, 64, isopo.BF16) == []
+
+
+@pytest.mark.parametrize("n,d_out", ((1 << 30, 1 << 20), ((1 << 31) - 1, 1 << 21), (1 << 29, 1 << 21), ((1 << 31) - 1, (1 << 22) - 8), ((1 << 31) - 1, 8),
+                                     (1 << 28, 4096)))
+def test_the_workspace_of_the_largest_layers(n, d_out):
+    """Rows per chunk of db's sums, 1024 workgroups of 256 columns over all of them, may pass 2^31."""
+    rows = -(-n * -(-d_out // 256) // 1024)
+    chunks = -(-n // (-(-rows // 8) * 8))
+    need = isopo.load().isopo_linear_backward_workspace(n, 8, d_out, isopo.BF16)
+    assert need == (chunks * d_out * 4 if chunks > 1 else 0)
