@@ -673,19 +673,34 @@ def _dtype_of(t: torch.Tensor, where: str) -> int:
     return code
 
 
-def _stream_for(stream, t: torch.Tensor) -> int:
-    """The given stream, or the current one of the tensor's device."""
-    return torch._C._cuda_getCurrentRawStream(t.get_device()) if stream is None else _stream(stream)
+def _stream_of(t: torch.Tensor) -> int:
+    """The current stream of the tensor's GPU."""
+    return torch._C._cuda_getCurrentRawStream(t.get_device())
 
 
-def _workspace(given: Optional[torch.Tensor], need: int, like: torch.Tensor, stream):
+def _under(stream, t: torch.Tensor, call, *args):
+    """call(*args) with `stream` as the current one, so that what it allocates is that stream's: memory that the caller's stream still works
+    on is not written, and what the call lets go is not handed to the caller's stream.  What it returns is not handed out
+    again before the caller's stream, too, is through with what it had been given by then."""
+    _on_one_device(t)
+    if not isinstance(stream, torch.cuda.Stream):
+        handle = _stream(stream)
+        stream = torch.cuda.ExternalStream(handle, device=t.device) if handle else torch.cuda.default_stream(t.device)
+    caller = torch.cuda.current_stream(t.device)
+    with torch.cuda.stream(stream):
+        out = call(*args)
+    for made in out.values() if isinstance(out, dict) else out if isinstance(out, tuple) else (out,):
+        if made is not None:
+            made.record_stream(caller)
+    return out
+
+
+def _workspace(given: Optional[torch.Tensor], need: int, like: torch.Tensor):
     """(pointer, bytes, what keeps it alive until the launches) of a call's workspace."""
     if given is None:
         if not need:
             return None, 0, None
         given = torch.empty(need, dtype=torch.uint8, device=like.device)
-        if stream is not None:              # the allocator takes it to be the current stream's
-            given.record_stream(stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(_stream(stream), device=like.device))
     return given.data_ptr(), given.numel() * given.element_size(), given
 
 
@@ -728,6 +743,8 @@ def linear(X: torch.Tensor, W: torch.Tensor, bias: Optional[torch.Tensor] = None
     """Y [n, d_out] = act(X W^T + bias) + residual, rounded once, for X [n, d_in] and W [d_out, d_in] (as nn.Linear holds it).
     X, residual and Y may have rows further apart than their length.  keep_z: returns (Y, Z), Z what the activation was applied
     to, for linear_backward.  act: "none", "relu", "gelu" (tanh form), "silu"."""
+    if stream is not None:
+        return _under(stream, X, linear, X, W, bias, act, residual, keep_z, Y, workspace)
     dtype, dt = _dtype_of(X, "linear"), X.dtype
     (n, d_in), (d_out, k) = X.shape, W.shape
     if k != d_in or W.dtype is not dt or not W.is_contiguous():
@@ -744,9 +761,9 @@ def linear(X: torch.Tensor, W: torch.Tensor, bias: Optional[torch.Tensor] = None
     _on_one_device(X, W, bias, residual, Y, workspace)
     Z = X.new_empty((n, d_out)) if keep_z else None
     lib = _lib or load()
-    ws, ws_bytes, keep = _workspace(workspace, _linear_workspace(n, d_in, d_out, dtype), X, stream)
+    ws, ws_bytes, keep = _workspace(workspace, _linear_workspace(n, d_in, d_out, dtype), X)
     layer = _LinearLayer(X.data_ptr(), W.data_ptr(), _ptr(bias), _ptr(residual), dtype, _act(act), n, d_in, d_out, ldx, ldr, ldy)
-    _check(lib.isopo_linear(layer, Y.data_ptr(), _ptr(Z), ws, ws_bytes, _stream_for(stream, X)), "isopo_linear")
+    _check(lib.isopo_linear(layer, Y.data_ptr(), _ptr(Z), ws, ws_bytes, _stream_of(X)), "isopo_linear")
     return (Y, Z) if keep_z else Y
 
 
@@ -754,6 +771,8 @@ def linear_backward(dY: torch.Tensor, W: torch.Tensor, Z: Optional[torch.Tensor]
                     need_db: bool = False, workspace: Optional[torch.Tensor] = None, stream=None):
     """(Delta, dX, db) of linear(): Delta = dY act'(Z), the Delta of a Layer; dX = Delta W; db [d_out] fp32 = the sum of Delta over
     the tokens.  What is not needed is None.  act "none": Delta is dY itself."""
+    if stream is not None:
+        return _under(stream, dY, linear_backward, dY, W, Z, act, need_dx, need_db, workspace)
     dtype, dt = _dtype_of(dY, "linear_backward"), dY.dtype
     n, (d_out, d_in) = dY.shape[0], W.shape
     lddy = _pitch(dY, "dY", dt, n, d_out)
@@ -768,9 +787,9 @@ def linear_backward(dY: torch.Tensor, W: torch.Tensor, Z: Optional[torch.Tensor]
     dX = dY.new_empty((n, d_in)) if need_dx else None
     db = torch.empty(d_out, dtype=torch.float32, device=dY.device) if need_db else None
     lib = _lib or load()
-    ws, ws_bytes, keep = _workspace(workspace, _linear_backward_workspace(n, d_in, d_out, dtype), dY, stream)
+    ws, ws_bytes, keep = _workspace(workspace, _linear_backward_workspace(n, d_in, d_out, dtype), dY)
     _check(lib.isopo_linear_backward(dY.data_ptr(), lddy, W.data_ptr(), _ptr(Z), dtype, code, n, d_in, d_out, _ptr(Delta), _ptr(dX),
-                                     _ptr(db), ws, ws_bytes, _stream_for(stream, dY)), "isopo_linear_backward")
+                                     _ptr(db), ws, ws_bytes, _stream_of(dY)), "isopo_linear_backward")
     return (dY if Delta is None else Delta), dX, db
 
 
@@ -796,6 +815,8 @@ def token_logprob(logits: torch.Tensor, targets: torch.Tensor, inv_temperature: 
     """logp [n], fp32, of the targets (int32, negative: a padded row) under softmax(inv_temperature * logits), and lse [n, 2] for
     token_logprob_backward: the largest logit and the logarithm of the sum over it (log-sum-exp = inv_temperature lse[:, 0] + lse[:, 1]).
     With `entropy` the entropy [n] too; with `weight` [n] also dlogits, the gradient of sum_t weight_t logp_t (dlogits=logits: in place)."""
+    if stream is not None:
+        return _under(stream, logits, token_logprob, logits, targets, inv_temperature, weight, entropy, dlogits)
     arg, n = _token_logits(logits, targets, inv_temperature, "token_logprob")
     dev = logits.device
     logp = torch.empty(n, dtype=torch.float32, device=dev)
@@ -814,7 +835,7 @@ def token_logprob(logits: torch.Tensor, targets: torch.Tensor, inv_temperature: 
     elif dlogits is not None:
         raise ValueError("dlogits needs weight")
     _on_one_device(logits, targets, weight, dlogits)
-    _check((_lib or load()).isopo_token_logprob(arg, logp.data_ptr(), lse.data_ptr(), _ptr(ent), w, d, ldd, _stream_for(stream, logits)),
+    _check((_lib or load()).isopo_token_logprob(arg, logp.data_ptr(), lse.data_ptr(), _ptr(ent), w, d, ldd, _stream_of(logits)),
            "isopo_token_logprob")
     return out
 
@@ -823,6 +844,8 @@ def token_logprob_backward(logits: torch.Tensor, targets: torch.Tensor, lse: tor
                            inv_temperature: float = 1.0, entropy: Optional[torch.Tensor] = None,
                            grad_entropy: Optional[torch.Tensor] = None, dlogits: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """The gradient in the logits from those of logp and (with `entropy`, as token_logprob returned it) of the entropy."""
+    if stream is not None:
+        return _under(stream, logits, token_logprob_backward, logits, targets, lse, grad_logp, inv_temperature, entropy, grad_entropy, dlogits)
     arg, n = _token_logits(logits, targets, inv_temperature, "token_logprob_backward")
     if lse.dtype is not torch.float32 or lse.shape != (n, 2) or not lse.is_contiguous():
         raise ValueError("lse must be what token_logprob returned, a contiguous fp32 tensor with two entries per token")
@@ -834,12 +857,14 @@ def token_logprob_backward(logits: torch.Tensor, targets: torch.Tensor, lse: tor
     _on_one_device(logits, targets, lse, grad_logp, entropy, grad_entropy, dlogits)
     _check((_lib or load()).isopo_token_logprob_backward(arg, lse.data_ptr(), _per_token(grad_logp, n, "grad_logp"),
                                                          _per_token(entropy, n, "entropy"), _per_token(grad_entropy, n, "grad_entropy"),
-                                                         dlogits.data_ptr(), ldd, _stream_for(stream, logits)), "isopo_token_logprob_backward")
+                                                         dlogits.data_ptr(), ldd, _stream_of(logits)), "isopo_token_logprob_backward")
     return dlogits
 
 
 def adamw_state(m: torch.Tensor, m_scale: torch.Tensor, v: torch.Tensor, v_scale: torch.Tensor, dtype=torch.float32, stream=None):
     """(m, v): the values that 8-bit states stand for."""
+    if stream is not None:
+        return _under(stream, m, adamw_state, m, m_scale, v, v_scale, dtype)
     n = m.numel()
     for name, code, scale in (("m", m, m_scale), ("v", v, v_scale)):
         if code.dtype != torch.uint8 or not code.is_contiguous() or code.numel() != n:
@@ -849,7 +874,7 @@ def adamw_state(m: torch.Tensor, m_scale: torch.Tensor, v: torch.Tensor, v_scale
     _on_one_device(m, m_scale, v, v_scale)
     out = [torch.empty(m.shape, dtype=dtype, device=m.device) for _ in range(2)]
     _check(load().isopo_adamw_state(m.data_ptr(), m_scale.data_ptr(), v.data_ptr(), v_scale.data_ptr(), n, _dtype_of(out[0], "adamw_state"),
-                                    out[0].data_ptr(), out[1].data_ptr(), _stream_for(stream, m)), "isopo_adamw_state")
+                                    out[0].data_ptr(), out[1].data_ptr(), _stream_of(m)), "isopo_adamw_state")
     return out[0], out[1]
 
 
@@ -907,6 +932,8 @@ class AdamW:
         before is returned (fp32 scalar on the device; one that is not finite leaves parameters and states as they are).  seed: of
         the 8-bit states' rounding; None: the step's number."""
         grads = list(grads)
+        if stream is not None:
+            return _under(stream, self.params[0], self.step, grads, lr, max_norm, seed)
         if list(map(torch.Tensor.numel, grads)) != self._sizes:
             raise ValueError("grads: one per parameter and of its size")
         kinds = {g.dtype for g in grads}
@@ -916,7 +943,7 @@ class AdamW:
         if set(map(torch.Tensor.get_device, grads)) != {self._device}:
             raise ValueError("grads must be on the parameters' GPU")
         arr = self._pointers(*map(torch.Tensor.data_ptr, grads))
-        lib, args, s, norm = _lib or load(), self._args, _stream_for(stream, first), None
+        lib, args, s, norm = _lib or load(), self._args, _stream_of(first), None
         args.grad_dtype, args.lr, args.max_norm = dtype, float(lr), float(max_norm or 0.0)
         args.step += 1
         args.seed = (args.step if seed is None else int(seed)) & 0xffffffff
