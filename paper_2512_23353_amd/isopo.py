@@ -884,9 +884,13 @@ class AdamW:
     params   contiguous tensors of one dtype, fp32 or bf16, updated in place
     masters  fp32 tensors that are updated in their place, params being their rounded copies; None: no such copies
     state_bits  32: m and v in fp32;  8: in bytes with a scale per ADAMW_BLOCK elements (uint8 tensors, read back by adamw_state)
-    m, v, m_scales, v_scales  existing states (a checkpoint's); None: zeros
+    m, v, m_scales, v_scales  existing states (a checkpoint's), updated in place; None: zeros
     step     steps done so far
     maximize  the steps go along the gradients
+
+    A parameter may get other storage between steps (`p.data = ...`, a module's `to`), or its place in `params` another tensor of its size
+    and type: every step looks where its parameters are.  States and masters stay where they are: the attributes of these names are
+    views of them, to be read and written in place.
     """
 
     def __init__(self, params, masters=None, state_bits: int = 32, betas=(0.9, 0.999), eps: float = 1e-8, weight_decay: float = 0.01,
@@ -899,29 +903,55 @@ class AdamW:
         first = self.params[0]
         kind = torch.uint8 if state_bits == 8 else torch.float32
         blocks = [-(-p.numel() // ADAMW_BLOCK) for p in self.params]
-        made = lambda given, sizes, dt: list(given) if given is not None else [torch.zeros(s, dtype=dt, device=first.device) for s in sizes]  # noqa: E731
-        self._sizes = [p.numel() for p in self.params]
-        self.masters = None if masters is None else list(masters)
-        self.m, self.v = made(m, self._sizes, kind), made(v, self._sizes, kind)
-        self.m_scales = made(m_scales, blocks, torch.float32) if state_bits == 8 else None
-        self.v_scales = made(v_scales, blocks, torch.float32) if state_bits == 8 else None
-        for what, ts, sizes, dt in (("params", self.params, self._sizes, first.dtype), ("masters", self.masters, self._sizes, torch.float32),
-                                    ("m", self.m, self._sizes, kind), ("v", self.v, self._sizes, kind),
-                                    ("m_scales", self.m_scales, blocks, torch.float32), ("v_scales", self.v_scales, blocks, torch.float32)):
-            if ts is not None and ([t.numel() for t in ts] != sizes or any(t.dtype != dt or not t.is_contiguous() or
-                                                                           t.device != first.device for t in ts)):
-                raise ValueError(f"{what}: contiguous {dt} tensors on one device, one per parameter and of its size, are needed")
-        n, self._device = len(self.params), first.get_device()
-        self._n = n
+        made = lambda given, sizes, dt: given if given is not None else [torch.zeros(s, dtype=dt, device=first.device) for s in sizes]  # noqa: E731
+        self._sizes, self._dtype, self._device = [p.numel() for p in self.params], first.dtype, first.device
+        self._device_index = first.get_device()
+        # the library is told addresses: what it is told of is held by tensors of this object's own, which nobody gives other storage
+        own = lambda what, ts, sizes, dt: tuple(t.detach() for t in self._fit(what, list(ts), sizes, dt))  # noqa: E731
+        self._states = {"m": own("m", made(m, self._sizes, kind), self._sizes, kind), "v": own("v", made(v, self._sizes, kind), self._sizes, kind)}
+        if masters is not None:
+            self._states["masters"] = own("masters", masters, self._sizes, torch.float32)
+        if state_bits == 8:
+            for name, given in (("m_scales", m_scales), ("v_scales", v_scales)):
+                self._states[name] = own(name, made(given, blocks, torch.float32), blocks, torch.float32)
+        self._n = n = len(self.params)
         none = [None] * n
-        self._tensors = (_AdamwTensor * n)(*[_AdamwTensor(p.data_ptr(), _ptr(w), a.data_ptr(), b.data_ptr(), _ptr(c), _ptr(d), p.numel())
-                                             for p, w, a, b, c, d in zip(self.params, self.masters or none, self.m, self.v,
-                                                                         self.m_scales or none, self.v_scales or none)])
+        at = lambda name: self._states.get(name, none)  # noqa: E731
+        self._tensors = (_AdamwTensor * n)(*[_AdamwTensor(None, _ptr(w), a.data_ptr(), b.data_ptr(), _ptr(c), _ptr(d), k)
+                                             for w, a, b, c, d, k in zip(at("masters"), at("m"), at("v"), at("m_scales"), at("v_scales"), self._sizes)])
+        self._param_at = None
+        self._find_params()
         self._pointers = ctypes.c_void_p * n
         self._args = _AdamwParams(_dtype_of(first, "AdamW"), F32, state_bits, int(bool(maximize)), 0.0, float(betas[0]), float(betas[1]), float(eps),
                                   float(weight_decay), 0.0, int(step), 0)
         need = int(load().isopo_grad_norm_workspace(self._tensors, n))
         self._norm_ws = torch.empty(max(need, 256), dtype=torch.uint8, device=first.device)
+
+    def _fit(self, what: str, ts: list, sizes: list, dtype: torch.dtype) -> list:
+        if [t.numel() for t in ts] != sizes or any(t.dtype != dtype or not t.is_contiguous() or t.device != self._device for t in ts):
+            raise ValueError(f"{what}: contiguous {dtype} tensors on one device, one per parameter and of its size, are needed")
+        return ts
+
+    def _find_params(self) -> None:
+        """The library's table of tensors, where a parameter is not where it was."""
+        at = list(map(torch.Tensor.data_ptr, self.params))
+        if at == self._param_at:
+            return
+        self._fit("params", self.params, self._sizes, self._dtype)
+        self._param_held = [p.detach() for p in self.params]         # until the next step: no other tensor comes to lie there meanwhile
+        for t, where in zip(self._tensors, at):
+            t.param = where
+        self._param_at = at
+
+    def _views(self, name: str):
+        ts = self._states.get(name)
+        return None if ts is None else tuple(t.detach() for t in ts)
+
+    masters = property(lambda self: self._views("masters"))
+    m = property(lambda self: self._views("m"))
+    v = property(lambda self: self._views("v"))
+    m_scales = property(lambda self: self._views("m_scales"))
+    v_scales = property(lambda self: self._views("v_scales"))
 
     @property
     def steps_done(self) -> int:
@@ -940,8 +970,9 @@ class AdamW:
         if len(kinds) != 1 or not all(map(torch.Tensor.is_contiguous, grads)):
             raise ValueError("grads must be contiguous and of one dtype")
         first, dtype = grads[0], _dtype_of(grads[0], "AdamW")
-        if set(map(torch.Tensor.get_device, grads)) != {self._device}:
+        if set(map(torch.Tensor.get_device, grads)) != {self._device_index}:
             raise ValueError("grads must be on the parameters' GPU")
+        self._find_params()
         arr = self._pointers(*map(torch.Tensor.data_ptr, grads))
         lib, args, s, norm = _lib or load(), self._args, _stream_of(first), None
         args.grad_dtype, args.lr, args.max_norm = dtype, float(lr), float(max_norm or 0.0)

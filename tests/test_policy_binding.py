@@ -8,3 +8,73 @@ from paper_2512_23353_amd import isopo
 def test_a_stream_for_host_tensors_is_refused():
     with pytest.raises(ValueError):
         isopo.linear(torch.zeros(4, 16), torch.zeros(8, 16), stream=1)
+
+
+class _Library:
+    """Takes note of the parameters' addresses that a step names, and launches nothing."""
+
+    def __init__(self, library):
+        self.library, self.params = library, []
+
+    def __getattr__(self, name):
+        if name in ("isopo_adamw", "isopo_adamw_clipped"):
+            return lambda tensors, grads, n, *rest: self.params.append([t.param for t in tensors[:n]]) or 0
+        return getattr(self.library, name)
+
+
+@pytest.fixture
+def library(monkeypatch):
+    """Host tensors pass for a GPU's, and the library is not called."""
+    lib = _Library(isopo.load())
+    monkeypatch.setattr(isopo, "_lib", lib)
+    monkeypatch.setattr(isopo, "_stream_of", lambda t: 0)
+    monkeypatch.setattr(torch.Tensor, "get_device", lambda t: 0)
+    return lib
+
+
+def _where(*params):
+    return [p.data_ptr() for p in params]
+
+
+def test_adamw_follows_its_parameters(library):
+    a, b = torch.nn.Parameter(torch.ones(64)), torch.nn.Parameter(torch.ones(8, 4))
+    opt = isopo.AdamW([a, b])
+    g = [torch.ones(64), torch.ones(8, 4)]
+    opt.step(g, 1e-3)
+    assert library.params[-1] == _where(a, b)
+    before = a.data_ptr()
+    a.data = torch.full((64,), 2.0)
+    opt.step(g, 1e-3, max_norm=1.0)
+    assert a.data_ptr() != before and library.params[-1] == _where(a, b)
+    c = torch.nn.Parameter(torch.zeros(8, 4))
+    opt.params[1] = c
+    opt.step(g, 1e-3)
+    assert library.params[-1] == _where(a, c) and opt.steps_done == 3
+    for bad in (torch.zeros(65), torch.zeros(64, dtype=torch.bfloat16), torch.zeros(128)[::2]):
+        a.data = bad
+        with pytest.raises(ValueError):
+            opt.step(g, 1e-3)
+    assert len(library.params) == 3 and opt.steps_done == 3
+
+
+def test_adamw_holds_what_the_library_is_told_of(library):
+    """A parameter's storage is not handed out again before the next step has looked; states are the optimiser's."""
+    p = torch.nn.Parameter(torch.ones(1 << 20))
+    opt = isopo.AdamW([p], state_bits=8)
+    old = p.data_ptr()
+    p.data = torch.empty(0)
+    assert all(torch.empty(1 << 20).data_ptr() != old for _ in range(4))
+    state = opt.m[0]
+    at = state.data_ptr()
+    state.data = torch.empty(0)
+    del state
+    assert opt.m[0].data_ptr() == at == opt._tensors[0].m
+    with pytest.raises(TypeError):
+        opt.m[0] = torch.zeros(1 << 20, dtype=torch.uint8)
+    with pytest.raises(AttributeError):
+        opt.v = []
+    opt.m_scales[0].fill_(2.0)
+    assert bool((opt.m_scales[0] == 2.0).all()) and opt.masters is None
+    given = torch.zeros(100)
+    opt = isopo.AdamW([torch.zeros(100)], m=[given], v=[torch.zeros(100)])
+    assert opt.m[0].data_ptr() == given.data_ptr()
