@@ -906,6 +906,8 @@ class AdamW:
         made = lambda given, sizes, dt: given if given is not None else [torch.zeros(s, dtype=dt, device=first.device) for s in sizes]  # noqa: E731
         self._sizes, self._dtype, self._device = [p.numel() for p in self.params], first.dtype, first.device
         self._device_index = first.get_device()
+        dtype = _dtype_of(first, "AdamW")
+        _on_one_device(first)
         # the library is told addresses: what it is told of is held by tensors of this object's own, which nobody gives other storage
         own = lambda what, ts, sizes, dt: tuple(t.detach() for t in self._fit(what, list(ts), sizes, dt))  # noqa: E731
         self._states = {"m": own("m", made(m, self._sizes, kind), self._sizes, kind), "v": own("v", made(v, self._sizes, kind), self._sizes, kind)}
@@ -922,7 +924,7 @@ class AdamW:
         self._param_at = None
         self._find_params()
         self._pointers = ctypes.c_void_p * n
-        self._args = _AdamwParams(_dtype_of(first, "AdamW"), F32, state_bits, int(bool(maximize)), 0.0, float(betas[0]), float(betas[1]), float(eps),
+        self._args = _AdamwParams(dtype, F32, state_bits, int(bool(maximize)), 0.0, float(betas[0]), float(betas[1]), float(eps),
                                   float(weight_decay), 0.0, int(step), 0)
         need = int(load().isopo_grad_norm_workspace(self._tensors, n))
         self._norm_ws = torch.empty(max(need, 256), dtype=torch.uint8, device=first.device)

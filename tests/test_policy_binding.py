@@ -10,6 +10,12 @@ def test_a_stream_for_host_tensors_is_refused():
         isopo.linear(torch.zeros(4, 16), torch.zeros(8, 16), stream=1)
 
 
+@pytest.mark.parametrize("bits", (8, 32))
+def test_adamw_refuses_host_tensors(bits):
+    with pytest.raises(ValueError):
+        isopo.AdamW([torch.zeros(300), torch.zeros(5)], state_bits=bits)
+
+
 class _Library:
     """Takes note of the parameters' addresses that a step names, and launches nothing."""
 
