@@ -940,6 +940,12 @@ class AdamW:
         if at == self._param_at:
             return
         self._fit("params", self.params, self._sizes, self._dtype)
+        # (a master may be its parameter)
+        masters = [w for w, p in zip(self._states.get("masters", ()), self.params) if w.data_ptr() != p.data_ptr()]
+        states = [t for name, ts in self._states.items() if name != "masters" for t in ts]
+        spans = sorted((t.data_ptr(), t.numel() * t.element_size()) for t in [*self.params, *masters, *states] if t.numel())
+        if any(a + n > b for (a, n), (b, _) in zip(spans, spans[1:])):
+            raise ValueError("parameters and states must not share memory: workgroups would update it at once")
         self._param_held = [p.detach() for p in self.params]         # until the next step: no other tensor comes to lie there meanwhile
         for t, where in zip(self._tensors, at):
             t.param = where

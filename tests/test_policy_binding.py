@@ -84,3 +84,16 @@ def test_adamw_holds_what_the_library_is_told_of(library):
     given = torch.zeros(100)
     opt = isopo.AdamW([torch.zeros(100)], m=[given], v=[torch.zeros(100)])
     assert opt.m[0].data_ptr() == given.data_ptr()
+
+
+def test_adamw_refuses_memory_that_is_written_twice(library):
+    p, buf = torch.zeros(512), torch.zeros(1024)
+    for bad in (lambda: isopo.AdamW([p, p]), lambda: isopo.AdamW([buf[:600], buf[512:]]), lambda: isopo.AdamW([p], m=[buf[:512]], v=[buf[256:768]]),
+                lambda: isopo.AdamW([p], m=[p]), lambda: isopo.AdamW([buf[:512], buf[512:]], masters=[buf[512:], torch.zeros(512)])):
+        with pytest.raises(ValueError):
+            bad()
+    opt = isopo.AdamW([buf[:512], buf[512:], torch.zeros(0), torch.zeros(0)], masters=[buf[:512], torch.zeros(512), torch.zeros(0), torch.zeros(0)])
+    opt.params[1] = buf[256:768]
+    with pytest.raises(ValueError):
+        opt.step([torch.zeros(512), torch.zeros(512), torch.zeros(0), torch.zeros(0)], 1e-3)
+    assert not library.params
