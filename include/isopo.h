@@ -575,7 +575,10 @@ isopo_status isopo_token_logprob_backward(const isopo_token_logits* logits, cons
  * [0, 1 - C]: even steps near zero, steps of one sixteenth of an octave above.  m: bit 7 is the sign, C = 17/16 2^-8.  v is held as its
  * square root, C = 17/16 2^-16.  Rounding to a step is up or down with the odds of what lies between (a hash of `seed`, the tensor's place in
  * the list and the element's index decides), so that a trailing mean with beta2 = 0.999, whose change in a step is far
- * smaller than a step of the code, moves as it should on average. */
+ * smaller than a step of the code, moves as it should on average.
+ *
+ * lr, step and seed are host values of the call: a captured call repeats that step at every replay, bias corrections and rounding
+ * included. */
 #define ISOPO_ADAMW_BLOCK 256
 typedef struct {
   void* param;                      /* [n] of param_dtype */

@@ -9,6 +9,7 @@ from __future__ import annotations
 import ctypes
 import functools
 import os
+import warnings
 from typing import Optional, Tuple
 
 import numpy as np
@@ -968,7 +969,10 @@ class AdamW:
     def step(self, grads, lr: float, max_norm: Optional[float] = None, seed: Optional[int] = None, stream=None) -> Optional[torch.Tensor]:
         """One step from `grads` (fp32 or bf16).  max_norm: they are scaled so that their common norm is at most that, and the norm
         before is returned (fp32 scalar on the device; one that is not finite leaves parameters and states as they are).  seed: of
-        the 8-bit states' rounding; None: the step's number."""
+        the 8-bit states' rounding; None: the step's number.
+
+        The step's number, lr and the seed are the call's, not the device's: a graph that captures it repeats THIS step, whatever number of
+        replays came before, which a warning says."""
         grads = list(grads)
         if stream is not None:
             return _under(stream, self.params[0], self.step, grads, lr, max_norm, seed)
@@ -981,6 +985,9 @@ class AdamW:
         if set(map(torch.Tensor.get_device, grads)) != {self._device_index}:
             raise ValueError("grads must be on the parameters' GPU")
         self._find_params()
+        if torch.cuda.is_current_stream_capturing():
+            warnings.warn(f"a graph that captures AdamW.step repeats step {self.steps_done + 1} at every replay: its bias corrections, lr and rounding "
+                          "do not move on", stacklevel=2)
         arr = self._pointers(*map(torch.Tensor.data_ptr, grads))
         lib, args, s, norm = _lib or load(), self._args, _stream_of(first), None
         args.grad_dtype, args.lr, args.max_norm = dtype, float(lr), float(max_norm or 0.0)

@@ -168,7 +168,10 @@ class PolicyTrainer:
                                      maximize=True)
 
     def step(self, lr: Optional[float] = None) -> Optional[torch.Tensor]:
-        """One step along the gradients gathered since the last; returns their norm (device) if it is limited."""
+        """One step along the gradients gathered since the last; returns their norm (device) if it is limited.  Not for a graph to capture:
+        replays would repeat this one step."""
+        if torch.cuda.is_current_stream_capturing():
+            raise RuntimeError("an optimiser step cannot be captured: replays would repeat it with its number, lr and rounding")
         grads = [getattr(layer, name + "_grad") for layer, name in self._slots]
         if any(g is None for g in grads):
             raise RuntimeError("a layer has no gradient: was it part of the backward pass?")

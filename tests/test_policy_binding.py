@@ -3,6 +3,7 @@ import pytest
 import torch
 
 from paper_2512_23353_amd import isopo
+from paper_2512_23353_amd.policy import PolicyLinear, PolicyTrainer
 
 
 def test_a_stream_for_host_tensors_is_refused():
@@ -35,6 +36,7 @@ def library(monkeypatch):
     monkeypatch.setattr(isopo, "_lib", lib)
     monkeypatch.setattr(isopo, "_stream_of", lambda t: 0)
     monkeypatch.setattr(torch.Tensor, "get_device", lambda t: 0)
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: False)
     return lib
 
 
@@ -97,3 +99,21 @@ def test_adamw_refuses_memory_that_is_written_twice(library):
     with pytest.raises(ValueError):
         opt.step([torch.zeros(512), torch.zeros(512), torch.zeros(0), torch.zeros(0)], 1e-3)
     assert not library.params
+
+
+def test_a_captured_step_says_that_it_repeats(library, monkeypatch, recwarn):
+    opt = isopo.AdamW([torch.zeros(64)], step=4)
+    opt.step([torch.zeros(64)], 1e-3)
+    assert not recwarn.list
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: True)
+    with pytest.warns(UserWarning, match="repeats step 6"):
+        opt.step([torch.zeros(64)], 1e-3)
+    layer = PolicyLinear(16, 8, dtype=torch.float32)
+    layer.weight_grad = torch.zeros(8, 16)
+    trainer = PolicyTrainer([layer])
+    with pytest.raises(RuntimeError, match="captured"):
+        trainer.step()
+    assert len(library.params) == 2 and trainer.optimiser.steps_done == 0 and layer.weight_grad is not None
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: False)
+    trainer.step()
+    assert trainer.optimiser.steps_done == 1
