@@ -575,7 +575,9 @@ isopo_status isopo_token_logprob_backward(const isopo_token_logits* logits, cons
  * [0, 1 - C]: even steps near zero, steps of one sixteenth of an octave above.  m: bit 7 is the sign, C = 17/16 2^-8.  v is held as its
  * square root, C = 17/16 2^-16.  Rounding to a step is up or down with the odds of what lies between (a hash of `seed`, the tensor's place in
  * the list and the element's index decides), so that a trailing mean with beta2 = 0.999, whose change in a step is far
- * smaller than a step of the code, moves as it should on average.
+ * smaller than a step of the code, moves as it should on average.  The largest magnitude of a block with a NaN is NaN: its states are then all NaN,
+ * and with an infinity infinite or NaN, as is the scale.  A gradient that is not finite thus spoils the next step of 256
+ * parameters where 32 bits spoil one; with max_norm it changes nothing at all.
  *
  * lr, step and seed are host values of the call: a captured call repeats that step at every replay, bias corrections and rounding
  * included. */

@@ -80,10 +80,15 @@ __device__ __forceinline__ unsigned encode(float x, float inv, unsigned u, unsig
   return code < most ? code : most;
 }
 
-__device__ __forceinline__ float wave_max(float x) {
+// The largest of a wave's magnitudes, by their bit patterns, which rise with them: a NaN's is above all others.
+__device__ __forceinline__ unsigned magnitude(float x) { return __builtin_bit_cast(unsigned, x) & 0x7fffffffu; }
+__device__ __forceinline__ float wave_largest(unsigned x) {
 #pragma unroll
-  for (int o = 32; o > 0; o >>= 1) x = fmaxf(x, __shfl_xor(x, o, 64));
-  return x;
+  for (int o = 32; o > 0; o >>= 1) {
+    const unsigned y = __shfl_xor(x, o, 64);
+    x = y > x ? y : x;
+  }
+  return __builtin_bit_cast(float, x);
 }
 
 template <bool BF16>
@@ -195,7 +200,8 @@ __global__ __launch_bounds__(256) void adamw_kernel(Params<BITS8> p) {
       v[q] = r * r;
     }
   }
-  float r[4], top_m = 0.f, top_r = 0.f;
+  float r[4];
+  unsigned most_m = 0, most_r = 0;
 #pragma unroll
   for (int q = 0; q < 4; ++q) {
     g[q] *= clip;
@@ -205,13 +211,12 @@ __global__ __launch_bounds__(256) void adamw_kernel(Params<BITS8> p) {
     if constexpr (BITS8) {
       if (q >= have) m[q] = v[q] = 0.f;
       r[q] = sqrtf(v[q]);
-      top_m = fmaxf(top_m, fabsf(m[q]));
-      top_r = fmaxf(top_r, r[q]);
+      most_m = magnitude(m[q]) > most_m ? magnitude(m[q]) : most_m;
+      most_r = magnitude(r[q]) > most_r ? magnitude(r[q]) : most_r;
     }
   }
   if constexpr (BITS8) {
-    top_m = wave_max(top_m);
-    top_r = wave_max(top_r);
+    const float top_m = wave_largest(most_m), top_r = wave_largest(most_r);
     const float m_inv = top_m > 0.f ? (1.f - kCm) / top_m : 0.f, v_inv = top_r > 0.f ? (1.f - kCv) / top_r : 0.f;
     mc = vc = 0;
 #pragma unroll

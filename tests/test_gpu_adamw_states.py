@@ -33,3 +33,43 @@ def test_a_captured_step_says_that_it_repeats(gpu_device):
         assert bool(((opt.m[0] - want).abs() <= 2.0 ** -20).all())
     trainer.step()
     assert trainer.optimiser.steps_done == 1 and layer.weight_grad is None
+
+
+@pytest.mark.parametrize("bad", (math.nan, math.inf, -math.inf))
+def test_a_gradient_that_is_not_finite_spoils_its_block_of_8_bit_states(gpu_device, bad):
+    """By the definition of a block's scale, its largest magnitude: no state of that block reads as a number.  Parameters of that step, and
+    all of the other blocks, are what they are without it; with a norm limit nothing changes."""
+    n, at = 1500, 700                                 # of six blocks the third
+    gen = torch.Generator(device=gpu_device).manual_seed(1)
+    w = torch.randn(n, generator=gen, device=gpu_device)
+    first, g = (torch.randn(n, generator=gen, device=gpu_device) for _ in range(2))
+    read = lambda o: isopo.adamw_state(o.m[0], o.m_scales[0], o.v[0], o.v_scales[0])  # noqa: E731
+
+    def run(grad, **kw):
+        opt = isopo.AdamW([w.clone()], state_bits=8)
+        opt.step([first], 1e-2, **kw)
+        opt.step([grad], 1e-2, **kw)
+        return opt
+
+    clean = run(g)
+    spoilt = g.clone()
+    spoilt[at] = bad
+    opt = run(spoilt)
+    block = slice(512, 768)
+    others = torch.ones(n, dtype=torch.bool, device=gpu_device)
+    others[block] = False
+    for got, want, scale, clean_scale in zip(read(opt), read(clean), (opt.m_scales[0], opt.v_scales[0]), (clean.m_scales[0], clean.v_scales[0])):
+        assert torch.equal(got[others], want[others]) and not torch.isfinite(got[block]).any()
+        assert torch.isnan(got[block]).sum() >= 255 and (not math.isnan(bad) or torch.isnan(got[block]).all())
+        assert not torch.isfinite(scale[2]) and torch.equal(torch.isnan(scale[2]), torch.tensor(math.isnan(bad), device=gpu_device))
+        assert torch.equal(scale[[0, 1, 3, 4, 5]], clean_scale[[0, 1, 3, 4, 5]])
+    one = torch.arange(n, device=gpu_device) == at
+    assert torch.isnan(opt.params[0][at]) and torch.equal(opt.params[0][~one], clean.params[0][~one])
+    # with 32 bits the element alone
+    wide = isopo.AdamW([w.clone()])
+    wide.step([spoilt], 1e-2)
+    assert torch.equal(torch.isfinite(wide.m[0]), ~one) and torch.equal(torch.isfinite(wide.params[0]), ~one)
+    limited, before = run(spoilt, max_norm=1e3), isopo.AdamW([w.clone()], state_bits=8)
+    before.step([first], 1e-2, max_norm=1e3)
+    for a, b in ((limited.params, before.params), (limited.m, before.m), (limited.v, before.v), (limited.m_scales, before.m_scales)):
+        assert torch.equal(a[0], b[0])
