@@ -27,6 +27,16 @@ from . import isopo
 from .hooks import VARIANTS, _hip_layer_step
 
 
+def _rows(t: torch.Tensor) -> torch.Tensor:
+    """t [n, d] as isopo.linear takes rows (contiguous, 16 bytes aligned, apart by whole vectors), or a copy that is: gradients of slices,
+    concatenations and broadcasts come as they may."""
+    vec = 16 // t.element_size()
+    apart = t.stride(0)
+    if (t.shape[1] > 1 and t.stride(1) != 1) or (t.shape[0] > 1 and (apart < t.shape[1] or apart % vec or apart >= 1 << 22)) or t.data_ptr() % 16:
+        return t.clone(memory_format=torch.contiguous_format)
+    return t
+
+
 class _Linear(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, weight, bias, residual, layer):
@@ -41,8 +51,7 @@ class _Linear(torch.autograd.Function):
     @once_differentiable
     def backward(ctx, dy):
         x, weight, z = ctx.saved_tensors
-        if dy.stride(-1) != 1 or dy.stride(0) < dy.shape[1]:         # an expanded gradient
-            dy = dy.contiguous()
+        dy = _rows(dy)
         delta, dx, db = isopo.linear_backward(dy, weight, z, ctx.layer.act, need_dx=ctx.needs_input_grad[0],
                                               need_db=ctx.has_bias and ctx.needs_input_grad[2])
         if ctx.needs_input_grad[1]:
@@ -80,9 +89,9 @@ class PolicyLinear(nn.Module):
             self.weight_grad += dw
 
     def forward(self, x: torch.Tensor, residual: Optional[torch.Tensor] = None) -> torch.Tensor:
-        rows = x.reshape(-1, x.shape[-1])
+        rows = _rows(x.reshape(-1, x.shape[-1]))
         if residual is not None:
-            residual = residual.reshape(-1, residual.shape[-1])
+            residual = _rows(residual.reshape(-1, residual.shape[-1]))
         y = _Linear.apply(rows, self.weight, self.bias, residual, self)
         return y.reshape(*x.shape[:-1], y.shape[-1])
 
@@ -109,6 +118,8 @@ class _TokenLogprob(torch.autograd.Function):
 def token_logprob(logits: torch.Tensor, targets: torch.Tensor, inv_temperature: float = 1.0, entropy: bool = False):
     """log-probabilities [n] (fp32) of the targets (int32 [n], negative: padding) under softmax(inv_temperature * logits), logits
     [n, vocab]; with `entropy` also the entropies [n].  Differentiable in the logits."""
+    if logits.stride(-1) != 1 or logits.stride(0) < logits.shape[1]:
+        logits = logits.contiguous()
     return _TokenLogprob.apply(logits, targets, float(inv_temperature), bool(entropy))
 
 

@@ -3,7 +3,7 @@ import pytest
 import torch
 
 from paper_2512_23353_amd import isopo
-from paper_2512_23353_amd.policy import PolicyLinear, PolicyTrainer
+from paper_2512_23353_amd.policy import PolicyLinear, PolicyTrainer, _rows
 
 
 def test_a_stream_for_host_tensors_is_refused():
@@ -117,3 +117,17 @@ def test_a_captured_step_says_that_it_repeats(library, monkeypatch, recwarn):
     monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: False)
     trainer.step()
     assert trainer.optimiser.steps_done == 1
+
+
+@pytest.mark.parametrize("dtype", (torch.float32, torch.bfloat16))
+def test_rows_are_taken_as_they_are_or_copied(dtype):
+    base = torch.arange(4096).to(dtype)
+    vec = 16 // base.element_size()
+    assert base.data_ptr() % 16 == 0
+    for t in (base[:256].view(4, 64), base.view(32, 128)[:, :64], base.view(32, 128)[:, vec:vec + 64], base.view(32, 128)[3:4, :64], base[:0].view(0, 64),
+              base[:1].view(1, 1).expand(1, 64).contiguous(), base[:7].view(7, 1)[:1]):
+        assert _rows(t) is t
+    for t in (base[1:257].view(4, 64), base[:64].view(1, 64).expand(4, 64), base.view(64, 64).t(), base[:4090].view(10, 409)[:, :64], base.view(32, 128)[:, 1:65],
+              base[:1].view(1, 1).expand(4, 64), base.as_strided((2, 8), (4, 1))):
+        got = _rows(t)
+        assert got is not t and got.is_contiguous() and got.data_ptr() % 16 == 0 and torch.equal(got, t)
