@@ -39,8 +39,9 @@ def _rows(t: torch.Tensor) -> torch.Tensor:
 
 class _Linear(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, x, weight, bias, residual, layer):
-        keep_z = layer.act != "none" and any(ctx.needs_input_grad)
+    def forward(ctx, x, weight, bias, residual, layer, recorded):
+        # (needs_input_grad is the tensors' own, whether autograd records or not)
+        keep_z = layer.act != "none" and recorded and any(ctx.needs_input_grad)
         out = isopo.linear(x, weight, bias, layer.act, residual, keep_z=keep_z)
         y, z = out if keep_z else (out, None)
         ctx.layer, ctx.has_bias, ctx.has_residual = layer, bias is not None, residual is not None
@@ -58,7 +59,7 @@ class _Linear(torch.autograd.Function):
             ctx.layer.add_weight_grad(x, delta)
         if db is not None:
             ctx.layer.bias_grad = db if ctx.layer.bias_grad is None else ctx.layer.bias_grad + db
-        return dx, None, None, dy if ctx.has_residual else None, None
+        return dx, None, None, dy if ctx.has_residual else None, None, None
 
 
 class PolicyLinear(nn.Module):
@@ -92,7 +93,7 @@ class PolicyLinear(nn.Module):
         rows = _rows(x.reshape(-1, x.shape[-1]))
         if residual is not None:
             residual = _rows(residual.reshape(-1, residual.shape[-1]))
-        y = _Linear.apply(rows, self.weight, self.bias, residual, self)
+        y = _Linear.apply(rows, self.weight, self.bias, residual, self, torch.is_grad_enabled())
         return y.reshape(*x.shape[:-1], y.shape[-1])
 
 

@@ -131,3 +131,25 @@ def test_rows_are_taken_as_they_are_or_copied(dtype):
               base[:1].view(1, 1).expand(4, 64), base.as_strided((2, 8), (4, 1))):
         got = _rows(t)
         assert got is not t and got.is_contiguous() and got.data_ptr() % 16 == 0 and torch.equal(got, t)
+
+
+def test_no_z_is_kept_where_nothing_is_recorded(monkeypatch):
+    kept = []
+
+    def linear(x, weight, bias, act, residual, keep_z):
+        kept.append(keep_z)
+        y = x @ weight.t()
+        return (y, y.clone()) if keep_z else y
+
+    monkeypatch.setattr(isopo, "linear", linear)
+    layer, x = PolicyLinear(16, 8, act="silu", dtype=torch.float32), torch.zeros(4, 16)
+    with torch.no_grad():
+        layer(x)
+    with torch.inference_mode():
+        layer(torch.zeros(4, 16))
+    layer(x)
+    layer.weight.requires_grad_(False)
+    layer(x)
+    layer(x.clone().requires_grad_())
+    PolicyLinear(16, 8, dtype=torch.float32)(x)
+    assert kept == [False, False, True, False, True, False]
