@@ -45,6 +45,7 @@ class _Linear(torch.autograd.Function):
         out = isopo.linear(x, weight, bias, layer.act, residual, keep_z=keep_z)
         y, z = out if keep_z else (out, None)
         ctx.layer, ctx.has_bias, ctx.has_residual = layer, bias is not None, residual is not None
+        ctx.mark = None if layer.update is None else layer.update.mark()
         ctx.save_for_backward(x, weight, z)
         return y
 
@@ -56,7 +57,7 @@ class _Linear(torch.autograd.Function):
         delta, dx, db = isopo.linear_backward(dy, weight, z, ctx.layer.act, need_dx=ctx.needs_input_grad[0],
                                               need_db=ctx.has_bias and ctx.needs_input_grad[2])
         if ctx.needs_input_grad[1]:
-            ctx.layer.add_weight_grad(x, delta)
+            ctx.layer.add_weight_grad(x, delta, ctx.mark)
         if db is not None:
             ctx.layer.bias_grad = db if ctx.layer.bias_grad is None else ctx.layer.bias_grad + db
         return dx, None, None, dy if ctx.has_residual else None, None, None
@@ -74,14 +75,14 @@ class PolicyLinear(nn.Module):
         self.weight = nn.Parameter(torch.empty((d_out, d_in), dtype=dtype, device=device))
         self.bias = nn.Parameter(torch.zeros(d_out, dtype=dtype, device=device)) if bias else None
         nn.init.normal_(self.weight, std=1.0 / math.sqrt(d_in))
-        self.update = None                  # (layer, X, Delta) -> dW; None: Delta^T X
+        self.update: Optional[IsopoUpdate] = None       # None: dW = Delta^T X
         self.weight_grad: Optional[torch.Tensor] = None
         self.bias_grad: Optional[torch.Tensor] = None
 
-    def add_weight_grad(self, x: torch.Tensor, delta: torch.Tensor) -> None:
+    def add_weight_grad(self, x: torch.Tensor, delta: torch.Tensor, mark: Optional[int] = None) -> None:
         x, delta = x.contiguous(), delta.contiguous()
         if self.update is not None:
-            dw = self.update(self, x, delta)
+            dw = self.update.layer_step(self, x, delta, mark)
         else:
             dw = isopo.weighted_grad(isopo.Layer(x, delta, [0, x.shape[0]]), None)
         if self.weight_grad is None:
@@ -140,16 +141,25 @@ class IsopoUpdate:
                     "ema_decay": float(ema_decay)}
         self._ema = {}
         self._offsets = self._advantages = None
+        self._begun, self._used = 0, False          # calls of begin(); whether a backward pass has been of the last one's sequences
         for layer in self.layers:
-            layer.update = self._layer_step
+            layer.update = self
 
     def begin(self, seq_offsets, advantages: torch.Tensor) -> None:
-        """The next backward passes are of these sequences: row offsets (host) and one fp32 advantage each (device)."""
+        """The next backward passes are of these sequences: row offsets (host) and one fp32 advantage each (device).  To be called before or after
+        the microbatch's forward pass; what runs forward once a backward pass has been of these sequences is another microbatch, which
+        needs its own."""
         self._offsets = np.ascontiguousarray(np.asarray(seq_offsets, dtype=np.int32))
         self._advantages = advantages
+        self._begun, self._used = self._begun + 1, False
 
-    def _layer_step(self, layer, x, delta):
-        if self._offsets is None:
+    def mark(self) -> int:
+        """The earliest call of begin() that a backward pass of what runs forward now can be of."""
+        return self._begun + self._used
+
+    def layer_step(self, layer, x, delta, mark: Optional[int] = None):
+        """dW of a layer's X and Delta; mark: what mark() said at its forward pass."""
+        if self._offsets is None or (mark is not None and self._begun < mark):
             raise RuntimeError("begin() tells which sequences a backward pass is of")
         if int(self._offsets[-1]) != x.shape[0]:
             raise ValueError(f"seq_offsets cover {int(self._offsets[-1])} tokens, the layer saw {x.shape[0]}")
@@ -158,7 +168,9 @@ class IsopoUpdate:
             if layer not in self._ema:
                 self._ema[layer] = torch.zeros(2, dtype=torch.float32, device=x.device)
             cfg = dict(cfg, ema_state=self._ema[layer])
-        return _hip_layer_step(x, delta, self._offsets, self._advantages, cfg)
+        dw = _hip_layer_step(x, delta, self._offsets, self._advantages, cfg)
+        self._used = True
+        return dw
 
     def remove(self) -> None:
         for layer in self.layers:

@@ -2,8 +2,8 @@
 import pytest
 import torch
 
-from paper_2512_23353_amd import isopo
-from paper_2512_23353_amd.policy import PolicyLinear, PolicyTrainer, _rows
+from paper_2512_23353_amd import isopo, policy
+from paper_2512_23353_amd.policy import IsopoUpdate, PolicyLinear, PolicyTrainer, _rows
 
 
 def test_a_stream_for_host_tensors_is_refused():
@@ -153,3 +153,44 @@ def test_no_z_is_kept_where_nothing_is_recorded(monkeypatch):
     layer(x.clone().requires_grad_())
     PolicyLinear(16, 8, dtype=torch.float32)(x)
     assert kept == [False, False, True, False, True, False]
+
+
+def test_a_backward_pass_is_of_sequences_that_were_named_for_it(monkeypatch):
+    """Offsets and advantages of the microbatch before are not taken for the next one's, whatever its number of tokens."""
+    steps = []
+
+    def layer_step(x, delta, offsets, advantages, cfg):
+        steps.append(advantages)
+        return delta.t() @ x
+
+    monkeypatch.setattr(policy, "_hip_layer_step", layer_step)
+    monkeypatch.setattr(isopo, "linear", lambda x, weight, *a, **kw: x.detach() @ weight.detach().t())
+    monkeypatch.setattr(isopo, "linear_backward", lambda dy, weight, *a, **kw: (dy, dy @ weight.detach(), None))
+    a, b = PolicyLinear(8, 8, dtype=torch.float32), PolicyLinear(8, 8, dtype=torch.float32)
+    update, x = IsopoUpdate([a, b]), torch.ones(4, 8)
+    one, two = torch.ones(1), torch.full((1,), 2.0)
+    with pytest.raises(RuntimeError, match="begin"):
+        b(a(x)).sum().backward()
+    loss = b(a(x)).sum()
+    update.begin([0, 4], one)                         # after the forward pass
+    loss.backward(retain_graph=True)
+    loss.backward()                                   # the same microbatch again
+    assert len(steps) == 4
+    loss = b(a(x)).sum()                              # another one
+    with pytest.raises(RuntimeError, match="begin"):
+        loss.backward(retain_graph=True)
+    assert len(steps) == 4
+    update.begin([0, 4], two)
+    loss.backward()
+    assert len(steps) == 6 and steps[-1] is two
+    update.begin([0, 4], one)                         # before the forward pass; a layer used twice
+    b(a(a(x))).sum().backward()
+    assert len(steps) == 9 and steps[-1] is one
+    first, second = b(a(x)).sum(), b(a(x)).sum()      # two forward, then two backward
+    update.begin([0, 4], one)
+    first.backward()
+    update.begin([0, 4], two)
+    second.backward()
+    assert [s is two for s in steps[-4:]] == [False, False, True, True]
+    update.remove()
+    b(a(x)).sum()
