@@ -923,7 +923,7 @@ class AdamW:
         self._tensors = (_AdamwTensor * n)(*[_AdamwTensor(None, _ptr(w), a.data_ptr(), b.data_ptr(), _ptr(c), _ptr(d), k)
                                              for w, a, b, c, d, k in zip(at("masters"), at("m"), at("v"), at("m_scales"), at("v_scales"), self._sizes)])
         self._param_at = None
-        self._find_params()
+        self.find_params()
         self._pointers = ctypes.c_void_p * n
         self._args = _AdamwParams(dtype, F32, state_bits, int(bool(maximize)), 0.0, float(betas[0]), float(betas[1]), float(eps),
                                   float(weight_decay), 0.0, int(step), 0)
@@ -935,8 +935,8 @@ class AdamW:
             raise ValueError(f"{what}: contiguous {dtype} tensors on one device, one per parameter and of its size, are needed")
         return ts
 
-    def _find_params(self) -> None:
-        """The library's table of tensors, where a parameter is not where it was."""
+    def find_params(self) -> None:
+        """Brings the library's table of tensors up to where the parameters are now; step() does so too."""
         at = list(map(torch.Tensor.data_ptr, self.params))
         if at == self._param_at:
             return
@@ -984,7 +984,7 @@ class AdamW:
         first, dtype = grads[0], _dtype_of(grads[0], "AdamW")
         if set(map(torch.Tensor.get_device, grads)) != {self._device_index}:
             raise ValueError("grads must be on the parameters' GPU")
-        self._find_params()
+        self.find_params()
         if torch.cuda.is_current_stream_capturing():
             warnings.warn(f"a graph that captures AdamW.step repeats step {self.steps_done + 1} at every replay: its bias corrections, lr and rounding "
                           "do not move on", stacklevel=2)

@@ -179,17 +179,46 @@ class IsopoUpdate:
 
 class PolicyTrainer:
     """AdamW on the layers' weights (and biases).  bf16 parameters get fp32 master copies.  The policy's objective is to be
-    maximised: the step goes along the gradients."""
+    maximised: the step goes along the gradients.
+
+    The parameters are the layers' at each step.  Where one was written or replaced since the last (a checkpoint loaded into it, other
+    storage or another Parameter), its master takes over what changed.  Writes through `.data` leave no trace on a parameter:
+    read_parameters() after them."""
 
     def __init__(self, layers: Iterable[PolicyLinear], lr: float = 1e-4, betas=(0.9, 0.999), eps: float = 1e-8, weight_decay: float = 0.0,
                  state_bits: int = 32, max_norm: Optional[float] = 1.0):
         self.layers = list(layers)
         self.lr, self.max_norm = float(lr), max_norm
         self._slots = [(layer, "weight") for layer in self.layers] + [(layer, "bias") for layer in self.layers if layer.bias is not None]
-        params = [getattr(layer, name).data for layer, name in self._slots]
-        masters = [p.float() for p in params] if params[0].dtype == torch.bfloat16 else None
-        self.optimiser = isopo.AdamW(params, masters=masters, state_bits=state_bits, betas=betas, eps=eps, weight_decay=weight_decay,
+        params = self._params()
+        self._masters = [p.detach().float() for p in params] if params[0].dtype == torch.bfloat16 else None
+        self.optimiser = isopo.AdamW(params, masters=self._masters, state_bits=state_bits, betas=betas, eps=eps, weight_decay=weight_decay,
                                      maximize=True)
+        self._seen = self._written(params)
+
+    def _params(self) -> list:
+        return [getattr(layer, name) for layer, name in self._slots]
+
+    @staticmethod
+    def _written(params) -> list:
+        """What differs where a parameter has been written or has other storage."""
+        return [(p.data_ptr(), p._version) for p in params]
+
+    def _follow(self, every: bool = False) -> list:
+        params = self.optimiser.params[:] = self._params()
+        self.optimiser.find_params()
+        now = self._written(params)
+        if self._masters is not None:
+            for p, master, seen, at in zip(params, self._masters, self._seen, now):
+                if every or seen != at:
+                    p, master = p.detach().reshape(-1), master.view(-1)
+                    master.copy_(torch.where(p == master.to(p.dtype), master, p.float()))        # what was not changed keeps its low bits
+        self._seen = now
+        return params
+
+    def read_parameters(self) -> None:
+        """The masters take over the parameters' values where these are not their rounded copies."""
+        self._follow(every=True)
 
     def step(self, lr: Optional[float] = None) -> Optional[torch.Tensor]:
         """One step along the gradients gathered since the last; returns their norm (device) if it is limited.  Not for a graph to capture:
@@ -199,6 +228,7 @@ class PolicyTrainer:
         grads = [getattr(layer, name + "_grad") for layer, name in self._slots]
         if any(g is None for g in grads):
             raise RuntimeError("a layer has no gradient: was it part of the backward pass?")
+        self._follow()
         norm = self.optimiser.step(grads, self.lr if lr is None else float(lr), max_norm=self.max_norm)
         for layer, name in self._slots:
             setattr(layer, name + "_grad", None)

@@ -59,3 +59,20 @@ def test_logits_of_any_strides(gpu_device):
         (token_logprob(view(a), y) * w).sum().backward()
         (torch.log_softmax(view(b), dim=1).gather(1, y.long()[:, None])[:, 0] * w).sum().backward()
         assert _rel(a.grad, b.grad) < 1e-5
+
+
+def test_a_loaded_checkpoint_stays_loaded(gpu_device):
+    """bf16 layers with fp32 masters: a step of learning rate 0 leaves what was loaded, and one moves from there."""
+    torch.manual_seed(2)
+    layer = PolicyLinear(64, 32, device=gpu_device)
+    trainer = PolicyTrainer([layer], weight_decay=0.0)
+    other = torch.randn(32, 64, device=gpu_device).bfloat16()
+    for load in (lambda: layer.load_state_dict({"weight": other}), lambda: setattr(layer, "weight", nn.Parameter(other.clone())),
+                 lambda: setattr(layer.weight, "data", other.clone()), lambda: (layer.weight.data.copy_(other), trainer.read_parameters())):
+        layer.weight_grad = torch.randn(32, 64, device=gpu_device)
+        trainer.step(lr=0.1)
+        assert not torch.equal(layer.weight, other)
+        load()
+        layer.weight_grad = torch.randn(32, 64, device=gpu_device)
+        trainer.step(lr=0.0)
+        assert torch.equal(layer.weight, other) and torch.equal(trainer.optimiser.masters[0], other.float())

@@ -194,3 +194,40 @@ def test_a_backward_pass_is_of_sequences_that_were_named_for_it(monkeypatch):
     assert [s is two for s in steps[-4:]] == [False, False, True, True]
     update.remove()
     b(a(x)).sum()
+
+
+def test_the_trainer_follows_its_layers(library):
+    """bf16 weights with fp32 masters; the library is not called, so parameters change from outside alone."""
+    torch.manual_seed(0)
+    a, b = PolicyLinear(16, 8), PolicyLinear(8, 16, bias=True)
+    trainer = PolicyTrainer([a, b])
+    low = [m * (1 + 2.0 ** -12) for m in trainer.optimiser.masters]
+    for m, value in zip(trainer.optimiser.masters, low):
+        m.copy_(value)                                # low bits that the parameters do not have
+
+    def step():
+        for layer, name in trainer._slots:
+            setattr(layer, name + "_grad", torch.zeros(getattr(layer, name).shape))
+        trainer.step()
+        assert library.params[-1] == _where(a.weight, b.weight, b.bias)
+        return trainer.optimiser.masters
+
+    assert all(torch.equal(m, v) for m, v in zip(step(), low))
+    loaded = {k: v.clone() for k, v in a.state_dict().items()}
+    loaded["weight"][0] = 3.0
+    a.load_state_dict(loaded)                         # a checkpoint, one row of which is new
+    masters = step()
+    assert bool((masters[0][0] == 3.0).all()) and torch.equal(masters[0][1:], low[0][1:]) and torch.equal(masters[1], low[1])
+    a.weight.data = a.weight.data.clone()             # other storage, the same values
+    assert torch.equal(step()[0], masters[0])
+    b.weight = torch.nn.Parameter(torch.full((16, 8), 5.0, dtype=torch.bfloat16))
+    masters = step()
+    assert bool((masters[1] == 5.0).all()) and torch.equal(masters[0][1:], low[0][1:])
+    b.bias.data.fill_(2.0)                            # leaves no trace
+    trainer.read_parameters()
+    assert bool((step()[2] == 2.0).all()) and torch.equal(step()[0][1:], low[0][1:])
+    a.to(torch.float32)
+    with pytest.raises(ValueError):
+        step()
+    with pytest.raises(ValueError):
+        PolicyTrainer([b, b])
