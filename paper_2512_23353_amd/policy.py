@@ -228,8 +228,11 @@ class PolicyTrainer:
         grads = [getattr(layer, name + "_grad") for layer, name in self._slots]
         if any(g is None for g in grads):
             raise RuntimeError("a layer has no gradient: was it part of the backward pass?")
-        self._follow()
+        params = self._follow()
         norm = self.optimiser.step(grads, self.lr if lr is None else float(lr), max_norm=self.max_norm)
+        # the library writes behind autograd's back: a backward pass of what ran forward with the old weights is refused, as after torch's own steps
+        torch.autograd.graph.increment_version(params)
+        self._seen = self._written(params)
         for layer, name in self._slots:
             setattr(layer, name + "_grad", None)
         return norm

@@ -231,3 +231,18 @@ def test_the_trainer_follows_its_layers(library):
         step()
     with pytest.raises(ValueError):
         PolicyTrainer([b, b])
+
+
+def test_a_backward_pass_through_weights_that_a_step_changed_is_refused(library, monkeypatch):
+    monkeypatch.setattr(isopo, "linear", lambda x, weight, *a, **kw: x.detach() @ weight.detach().t())
+    monkeypatch.setattr(isopo, "linear_backward", lambda dy, weight, *a, **kw: (dy, dy @ weight.detach(), None))
+    monkeypatch.setattr(isopo, "weighted_grad", lambda layer, c: layer.Delta.t() @ layer.X)
+    a, b = PolicyLinear(8, 8, dtype=torch.float32), PolicyLinear(8, 8, dtype=torch.float32)
+    trainer = PolicyTrainer([a, b])
+    for _ in range(2):
+        loss = b(a(torch.ones(4, 8))).sum()
+        loss.backward(retain_graph=True)
+        trainer.step()
+        with pytest.raises(RuntimeError, match="inplace"):
+            loss.backward()
+        a.weight_grad = b.weight_grad = None
