@@ -33,8 +33,8 @@ __device__ __forceinline__ float act_slope(float z) {
     return s + z * s * (1.f - s);
   }
   if constexpr (A == Act::kGelu) {
-    const float s = sigmoid(2.f * kGeluA * (z + kGeluB * z * z * z));
-    return s + z * s * (1.f - s) * (2.f * kGeluA) * (1.f + 3.f * kGeluB * z * z);
+    const float s = sigmoid(2.f * kGeluA * (z + kGeluB * z * z * z)), t = s * (1.f - s);
+    return t == 0.f ? s : s + z * t * (2.f * kGeluA) * (1.f + 3.f * kGeluB * z * z);          // (z^2 may leave fp32 where t is 0)
   }
   return 1.f;
 }
