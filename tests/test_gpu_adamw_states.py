@@ -73,3 +73,47 @@ def test_a_gradient_that_is_not_finite_spoils_its_block_of_8_bit_states(gpu_devi
     before.step([first], 1e-2, max_norm=1e3)
     for a, b in ((limited.params, before.params), (limited.m, before.m), (limited.v, before.v), (limited.m_scales, before.m_scales)):
         assert torch.equal(a[0], b[0])
+
+
+def _rounded(x, values, u):
+    """Magnitudes over their scale to the codes' values, up with the odds of what lies between where u is uniform, to the nearest where it is 1/2."""
+    lo = (torch.searchsorted(values, x, right=True) - 1).clamp(0, len(values) - 2)
+    part = (x - values[lo]) / (values[lo + 1] - values[lo])
+    return values[(lo + (part + u >= 1.0)).clamp_max(len(values) - 1)]
+
+
+def _held(x, c, values, u):
+    """Blocks of magnitudes as 8-bit states hold them."""
+    scale = x.amax(dim=1, keepdim=True) / (1 - c)
+    return _rounded(x / scale, values, u) * scale
+
+
+def test_trailing_means_in_8_bits_follow_beside_a_steady_maximum(gpu_device):
+    """The block's largest gradient stays, the others fall to a tenth after half of the steps: their codes themselves have to move, by about a
+    two-hundredth of a code a step.  Against a 64-bit model of the states with another source of uniform dither: over 65280 independent elements the
+    means of m and sqrt(v), each over what 64-bit states hold, differ by no more than 6 standard errors of the two.  The model that rounds to the
+    nearest code is far outside (its codes stay where they were)."""
+    blocks, steps, beta = 256, 200, 0.999
+    gen = torch.Generator().manual_seed(4)
+    g = torch.rand((blocks, 256), generator=gen) * 0.5 + 0.25
+    g[:, 0] = 1.0
+    late = torch.where(torch.arange(256) == 0, 1.0, 0.1) * g
+    opt = isopo.AdamW([torch.zeros(blocks * 256, device=gpu_device)], state_bits=8, betas=(beta, beta))
+    true_m, true_v = (torch.zeros((blocks, 256), dtype=torch.float64) for _ in range(2))
+    models = {"dither": [true_m.clone(), true_v.clone()], "nearest": [true_m.clone(), true_v.clone()]}
+    for t in range(steps):
+        x = (g if t < steps // 2 else late).double()
+        opt.step([x.float().reshape(-1).to(gpu_device)], 0.0)
+        true_m, true_v = beta * true_m + (1 - beta) * x, beta * true_v + (1 - beta) * x * x
+        for name, (m, v) in models.items():
+            u = [torch.rand((blocks, 256), generator=gen, dtype=torch.float64) if name == "dither" else 0.5 for _ in range(2)]
+            m, v = beta * m + (1 - beta) * x, beta * v + (1 - beta) * x * x
+            models[name] = [_held(m, ref.C_M, ref.M_VALUES, u[0]), _held(torch.sqrt(v), ref.C_V, ref.V_VALUES, u[1]) ** 2]
+    got = [s.double().cpu().view(blocks, 256) for s in isopo.adamw_state(opt.m[0], opt.m_scales[0], opt.v[0], opt.v_scales[0])]
+    share = lambda held: (held[0][:, 1:] / true_m[:, 1:], torch.sqrt(held[1][:, 1:] / true_v[:, 1:]))  # noqa: E731
+    for kernel, model, nearest in zip(share(got), share(models["dither"]), share(models["nearest"])):
+        error = math.sqrt(float(model.var() + kernel.var()) / model.numel())
+        assert error < 1e-3
+        assert abs(float(kernel.mean() - model.mean())) <= 6 * error, (float(kernel.mean()), float(model.mean()), error)
+        assert abs(float(nearest.mean() - model.mean())) > 100 * error
+        assert abs(float(model.mean()) - 1.0) <= 6 * error
