@@ -269,12 +269,7 @@ constexpr int kNormChunk = 16384;
 template <bool GB>
 __global__ __launch_bounds__(256) void grad_norm_kernel(NormParams p) {
   __shared__ double red[4];
-  int lo = 0, hi = p.n_tensors;
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1;
-    if (p.entry[mid].first <= blockIdx.x) lo = mid; else hi = mid;
-  }
-  const auto& e = p.entry[__builtin_amdgcn_readfirstlane(lo)];
+  const auto& e = p.entry[__builtin_amdgcn_readfirstlane(tensor_of(p, blockIdx.x))];
   const long long i0 = (long long)(blockIdx.x - e.first) * kNormChunk;
   const long long i1 = e.n - i0 > kNormChunk ? i0 + kNormChunk : e.n;
   float t = 0.f;
