@@ -879,6 +879,10 @@ def adamw_state(m: torch.Tensor, m_scale: torch.Tensor, v: torch.Tensor, v_scale
     return out[0], out[1]
 
 
+# attribute of AdamW -> column of the library's table of tensors
+_ADAMW_COLUMN = {"params": 0, "masters": 1, "m": 2, "v": 3, "m_scales": 4, "v_scales": 5, "n": 6}
+
+
 class AdamW:
     """AdamW over a list of tensors, all updated by one step() in few launches (isopo_adamw, isopo_adamw_clipped).
 
@@ -903,25 +907,28 @@ class AdamW:
             raise ValueError("state_bits must be 8 or 32")
         first = self.params[0]
         kind = torch.uint8 if state_bits == 8 else torch.float32
-        blocks = [-(-p.numel() // ADAMW_BLOCK) for p in self.params]
-        made = lambda given, sizes, dt: given if given is not None else [torch.zeros(s, dtype=dt, device=first.device) for s in sizes]  # noqa: E731
-        self._sizes, self._dtype, self._device = [p.numel() for p in self.params], first.dtype, first.device
-        self._device_index = first.get_device()
         dtype = _dtype_of(first, "AdamW")
         _on_one_device(first)
-        # the library is told addresses: what it is told of is held by tensors of this object's own, which nobody gives other storage
-        own = lambda what, ts, sizes, dt: tuple(t.detach() for t in self._fit(what, list(ts), sizes, dt))  # noqa: E731
-        self._states = {"m": own("m", made(m, self._sizes, kind), self._sizes, kind), "v": own("v", made(v, self._sizes, kind), self._sizes, kind)}
-        if masters is not None:
-            self._states["masters"] = own("masters", masters, self._sizes, torch.float32)
-        if state_bits == 8:
-            for name, given in (("m_scales", m_scales), ("v_scales", v_scales)):
-                self._states[name] = own(name, made(given, blocks, torch.float32), blocks, torch.float32)
+        self._dtype, self._device_index = first.dtype, first.get_device()
         self._n = n = len(self.params)
-        none = [None] * n
-        at = lambda name: self._states.get(name, none)  # noqa: E731
-        self._tensors = (_AdamwTensor * n)(*[_AdamwTensor(None, _ptr(w), a.data_ptr(), b.data_ptr(), _ptr(c), _ptr(d), k)
-                                             for w, a, b, c, d, k in zip(at("masters"), at("m"), at("v"), at("m_scales"), at("v_scales"), self._sizes)])
+        self._sizes = list(map(torch.Tensor.numel, self.params))
+        blocks = [-(-k // ADAMW_BLOCK) for k in self._sizes]
+        wanted = [("m", m, self._sizes, kind), ("v", v, self._sizes, kind)]
+        if masters is not None:
+            wanted.append(("masters", masters, self._sizes, torch.float32))
+        if state_bits == 8:
+            wanted += [("m_scales", m_scales, blocks, torch.float32), ("v_scales", v_scales, blocks, torch.float32)]
+        # The library is told addresses.  What lies there is held by tensors of this object's own, which nobody else can give other storage.
+        self._states = {}
+        self._table = np.zeros((n, len(_AdamwTensor._fields_)), dtype=np.int64)
+        self._table[:, _ADAMW_COLUMN["n"]] = self._sizes
+        for name, given, sizes, dt in wanted:
+            if given is None:
+                self._states[name] = [torch.zeros(k, dtype=dt, device=first.device) for k in sizes]
+            else:
+                self._states[name] = [t.data for t in self._fit(name, list(given), sizes, dt)]
+            self._table[:, _ADAMW_COLUMN[name]] = list(map(torch.Tensor.data_ptr, self._states[name]))
+        self._tensors = (_AdamwTensor * n).from_buffer(self._table)
         self._param_at = None
         self.find_params()
         self._pointers = ctypes.c_void_p * n
@@ -931,7 +938,8 @@ class AdamW:
         self._norm_ws = torch.empty(max(need, 256), dtype=torch.uint8, device=first.device)
 
     def _fit(self, what: str, ts: list, sizes: list, dtype: torch.dtype) -> list:
-        if [t.numel() for t in ts] != sizes or any(t.dtype != dtype or not t.is_contiguous() or t.device != self._device for t in ts):
+        if (list(map(torch.Tensor.numel, ts)) != sizes or {t.dtype for t in ts} != {dtype} or not all(map(torch.Tensor.is_contiguous, ts)) or
+                set(map(torch.Tensor.get_device, ts)) != {self._device_index}):
             raise ValueError(f"{what}: contiguous {dtype} tensors on one device, one per parameter and of its size, are needed")
         return ts
 
@@ -941,20 +949,24 @@ class AdamW:
         if at == self._param_at:
             return
         self._fit("params", self.params, self._sizes, self._dtype)
-        # (a master may be its parameter)
-        masters = [w for w, p in zip(self._states.get("masters", ()), self.params) if w.data_ptr() != p.data_ptr()]
-        states = [t for name, ts in self._states.items() if name != "masters" for t in ts]
-        spans = sorted((t.data_ptr(), t.numel() * t.element_size()) for t in [*self.params, *masters, *states] if t.numel())
-        if any(a + n > b for (a, n), (b, _) in zip(spans, spans[1:])):
+        starts, ends = [np.array(at, dtype=np.int64)], [np.array(at) + np.array(self._sizes) * self._dtype.itemsize]
+        for name, ts in self._states.items():
+            column = self._table[:, _ADAMW_COLUMN[name]]
+            mine = column != starts[0] if name == "masters" else column != 0          # (a master may be its parameter)
+            starts.append(column[mine])
+            ends.append((column + np.array([t.numel() * t.element_size() for t in ts]))[mine])
+        starts, ends = np.concatenate(starts), np.concatenate(ends)
+        starts, ends = starts[ends > starts], ends[ends > starts]
+        order = np.argsort(starts)
+        if bool((ends[order][:-1] > starts[order][1:]).any()):
             raise ValueError("parameters and states must not share memory: workgroups would update it at once")
-        self._param_held = [p.detach() for p in self.params]         # until the next step: no other tensor comes to lie there meanwhile
-        for t, where in zip(self._tensors, at):
-            t.param = where
+        self._param_held = [p.untyped_storage() for p in self.params]          # until the next step: nothing else comes to lie there meanwhile
+        self._table[:, _ADAMW_COLUMN["params"]] = at
         self._param_at = at
 
     def _views(self, name: str):
         ts = self._states.get(name)
-        return None if ts is None else tuple(t.detach() for t in ts)
+        return None if ts is None else tuple(t.data for t in ts)
 
     masters = property(lambda self: self._views("masters"))
     m = property(lambda self: self._views("m"))
