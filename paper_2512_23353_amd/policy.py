@@ -45,7 +45,8 @@ class _Linear(torch.autograd.Function):
         out = isopo.linear(x, weight, bias, layer.act, residual, keep_z=keep_z)
         y, z = out if keep_z else (out, None)
         ctx.layer, ctx.has_bias, ctx.has_residual = layer, bias is not None, residual is not None
-        ctx.mark = None if layer.update is None else layer.update.mark()
+        mark = getattr(layer.update, "mark", None)
+        ctx.mark = mark and mark()
         ctx.save_for_backward(x, weight, z)
         return y
 
@@ -64,7 +65,8 @@ class _Linear(torch.autograd.Function):
 
 
 class PolicyLinear(nn.Module):
-    """act(x W^T + bias) + residual for x [..., d_in], a linear layer of the policy (isopo.linear).  After a backward pass
+    """act(x W^T + bias) + residual for x [..., d_in], a linear layer of the policy (isopo.linear).  d_in and d_out are multiples of 8 (bf16)
+    or 4 (fp32), as the layer step asks; a vocabulary of another size is padded to one.  After a backward pass
     `weight_grad` [d_out, d_in] and `bias_grad` [d_out] hold the gradients in fp32; the parameters' .grad stay as they are."""
 
     def __init__(self, d_in: int, d_out: int, bias: bool = False, act: str = "none", dtype=torch.bfloat16, device=None):
@@ -75,14 +77,14 @@ class PolicyLinear(nn.Module):
         self.weight = nn.Parameter(torch.empty((d_out, d_in), dtype=dtype, device=device))
         self.bias = nn.Parameter(torch.zeros(d_out, dtype=dtype, device=device)) if bias else None
         nn.init.normal_(self.weight, std=1.0 / math.sqrt(d_in))
-        self.update: Optional[IsopoUpdate] = None       # None: dW = Delta^T X
+        self.update = None                  # (layer, X, Delta) -> dW, or an IsopoUpdate; None: Delta^T X
         self.weight_grad: Optional[torch.Tensor] = None
         self.bias_grad: Optional[torch.Tensor] = None
 
     def add_weight_grad(self, x: torch.Tensor, delta: torch.Tensor, mark: Optional[int] = None) -> None:
         x, delta = x.contiguous(), delta.contiguous()
         if self.update is not None:
-            dw = self.update.layer_step(self, x, delta, mark)
+            dw = self.update(self, x, delta) if mark is None else self.update(self, x, delta, mark)
         else:
             dw = isopo.weighted_grad(isopo.Layer(x, delta, [0, x.shape[0]]), None)
         if self.weight_grad is None:
@@ -157,7 +159,7 @@ class IsopoUpdate:
         """The earliest call of begin() that a backward pass of what runs forward now can be of."""
         return self._begun + self._used
 
-    def layer_step(self, layer, x, delta, mark: Optional[int] = None):
+    def __call__(self, layer, x, delta, mark: Optional[int] = None):
         """dW of a layer's X and Delta; mark: what mark() said at its forward pass."""
         if self._offsets is None or (mark is not None and self._begun < mark):
             raise RuntimeError("begin() tells which sequences a backward pass is of")

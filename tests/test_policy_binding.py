@@ -164,6 +164,7 @@ def test_a_backward_pass_is_of_sequences_that_were_named_for_it(monkeypatch):
         return delta.t() @ x
 
     monkeypatch.setattr(policy, "_hip_layer_step", layer_step)
+    monkeypatch.setattr(isopo, "weighted_grad", lambda layer, c: layer.Delta.t() @ layer.X)
     monkeypatch.setattr(isopo, "linear", lambda x, weight, *a, **kw: x.detach() @ weight.detach().t())
     monkeypatch.setattr(isopo, "linear_backward", lambda dy, weight, *a, **kw: (dy, dy @ weight.detach(), None))
     a, b = PolicyLinear(8, 8, dtype=torch.float32), PolicyLinear(8, 8, dtype=torch.float32)
@@ -193,7 +194,10 @@ def test_a_backward_pass_is_of_sequences_that_were_named_for_it(monkeypatch):
     second.backward()
     assert [s is two for s in steps[-4:]] == [False, False, True, True]
     update.remove()
-    b(a(x)).sum()
+    b(a(x)).sum().backward()
+    a.update = lambda layer, x, delta: steps.append(layer) or delta.t() @ x
+    b(a(x)).sum().backward()
+    assert steps[-1] is a
 
 
 def test_the_trainer_follows_its_layers(library):
