@@ -607,8 +607,8 @@ size_t isopo_grad_norm_workspace(const isopo_adamw_tensor* tensors, int32_t n_te
 isopo_status isopo_grad_norm(const isopo_adamw_tensor* tensors, const void* const* grads, int32_t n_tensors, isopo_dtype grad_dtype,
                              float* norm, void* workspace, size_t ws_bytes, void* stream);
 
-/* tensors, grads: HOST arrays (grads: of device pointers, 16-byte aligned).  norm: device fp32 [1] or NULL.  A norm that is not
- * finite leaves every tensor as it is. */
+/* tensors, grads: HOST arrays (grads: of device pointers, 16-byte aligned).  What is written (param, master, m, v, scales) may not overlap
+ * but for master = param of fp32.  norm: device fp32 [1] or NULL.  A norm that is not finite leaves every tensor as it is. */
 isopo_status isopo_adamw(const isopo_adamw_tensor* tensors, const void* const* grads, int32_t n_tensors, const isopo_adamw_params* params,
                          const float* norm, void* stream);
 

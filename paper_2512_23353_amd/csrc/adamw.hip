@@ -1,8 +1,9 @@
 // AdamW over many tensors in few launches, with states in 32 or 8 bits; the norm of all gradients; the values of 8-bit states.
 //
 // Bound by HBM: every element is read and written once, 28 bytes (fp32) or 18 (bf16 parameter, fp32 master, 8-bit states,
-// fp32 gradient) of it.  218 M elements of the latter kind: 0.72 - 0.82 ms, 4.8 - 5.5 TB/s (a large copy: 4.9); the norm before it 0.18 ms, 4.9 TB/s; the
-// states' values as bf16 0.21 ms, 6.2 TB/s.  70 tensors of 4096 elements and so: 13 us in three launches.  The tensors' addresses travel in the kernel's
+// fp32 gradient) of it.  218 M elements, fp32: 1.14 ms, 5.3 TB/s, with the norm 1.32; the latter kind 0.72 - 0.82 ms, 4.8 - 5.5 TB/s (a large
+// copy: 4.9); the norm before it 0.18 ms, 4.9 TB/s; the states' values as bf16 0.21 ms, 6.2 TB/s.  70 tensors of 4096 elements and so: 12 us in two
+// launches, and the host's time, 30 us a step, hides them.  The tensors' addresses travel in the kernel's
 // arguments, 83 or 55 a launch: nothing is copied to the device and nothing waits.  A workgroup takes 1024 elements of one tensor, a vector a lane.
 //
 // 8-bit states: ISOPO_ADAMW_BLOCK = 256 elements share a scale; a wave holds such a block, four elements a lane, so its

@@ -9,8 +9,8 @@
 // are all latency), two stages of LDS, one barrier a stage.  A thread loads four terms of a row (X, Delta, W of the forward pass) or of a column
 // (W of dX = Delta W, whose rows are the sum's terms), splits them in registers and stores 8 bytes a part: units of 16 bytes hold eight terms
 // of a row and part, which is the MFMA's operand.  A step is multiplied while the next is split and stored and the one after it is on its way.
-// 9999 x 1536 -> 1536: 252 us, 187 TFLOP/s of fp32 products, 1.12 PFLOP/s of bf16 ones (a library's fp32 product of that size takes
-// 377 us); 2.9 rounds of workgroups, the last of them two thirds empty.
+// 9999 x 1536 -> 1536: 255 us, 185 TFLOP/s of fp32 products, 1.11 PFLOP/s of bf16 ones (a library's fp32 product of that size takes
+// 377 us); of its 948 workgroups 768, three to a unit, are a full round, and the other 180 are alone on theirs for the last quarter of the time.
 // Where even the 64 x 64 tiles are few and the sums long, four or eight waves split a tile's sum instead: they wait for none of the others
 // before its end, and fewer launches need parts in the workspace (2001 x 1220 -> 300 as dX 25.5 -> 18.8 us, 1024 x 1024 -> 1024 25.6 -> 19.8).
 // They are bound by the MFMAs and the splits, whose times add up on a SIMD (with no loads 51 of 61 us at 1024 x 4096 -> 1024).
@@ -550,7 +550,8 @@ constexpr int sum_waves_of(Tile t) { return t == Tile::k64By4 ? 4 : t == Tile::k
 // it takes of its compute unit: 128 x 128 tiles, three to a unit, 2 and 0.64 (alone 0.75); 64 x 64, 1 and 0.23 (alone 0.3); by four waves that split
 // the sum 2.5 (alone 1.5) and 0.79; by eight, where none waits for a unit, 1.5 and 1.45.  Parts cost a second launch, 0.12 each and the workspace's
 // traffic at 8 bytes per output and part (a little much beside the kernels' time, as the second launch costs the host more).  With 4 us for the
-// launch it is 14 % below to 28 % above what was measured on 40 products of 1 .. 40000 tokens.
+// launch it is 14 % below to 28 % above what was measured on 40 products of 1 .. 40000 tokens.  Past one full round it takes rounds as divisible,
+// which they are on many: a few workgroups behind a full round cost more than it says (9999 x 1536 -> 1536: 235 modelled, 255 measured).
 LinearPlan plan(long long rows, int k, int n_out, bool may_split) {
   const int blocks = (k + kTerms - 1) / kTerms;
   const double outputs = (double)rows * n_out;
